@@ -303,6 +303,120 @@ mfmg_status mfmg_meta_grad_noalloc(mfmg_problem_t problem, const float* theta0,
                                    const mfmg_batch* val_batch, float* d_eta_out,
                                    float* val_loss_out, size_t* peak_bytes_out, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Operators of a decoder's attention, primal and dual.  A decoder problem with
+ * grouped heads, query/key norms, packed documents or the rotary options runs
+ * these same kernels; callers with a model of their own reach them here.
+ *
+ * Rows are by token: row i of an array holds the values of token i, its heads side
+ * by side (head h at columns h * head_dim).  A QKV row is q heads | k heads | v
+ * heads, (heads + 2 kv_heads) * head_dim columns; query head h reads key head
+ * h / (heads / kv_heads).  Leading dimensions count elements; row pointers and rows
+ * must be 16-byte aligned.  T is the operand type: bfloat16 (MFMG_PREC_BF16) or
+ * float32; gains and the rows that enter the rotation are float32, sums are float32.
+ * Tangents (names ending in d, and xd / dxd structs) are given together or not at
+ * all: with them a call also returns the derivative of its outputs along them.
+ *
+ * Tokens of several sequences lie behind one another: a plan made from their offsets
+ * (mfmg_seq_plan) says which token belongs to which sequence.  Tokens before the first
+ * or behind the last one are unused rows: nothing of them enters a result (they may
+ * hold anything) and output rows of theirs stay as they were.  Nothing of one sequence
+ * enters another's results either, NaN and infinities included.
+ */
+/* How rotary frequencies theta_j = rope_base^(-2j / rope_dims), j < rope_dims / 2, are
+ * stretched for contexts longer than those trained on, by rope_factor f >= 1:
+ * PLAIN not; LINEAR theta_j / f; BASE with rope_base * f^(D / (D - 2)), D = rope_dims
+ * (>= 4); PARTS theta_j ((1 - w) / f + w), w = clamp((t - rope_slow) / (rope_fast -
+ * rope_slow), 0, 1), t = rope_train_len theta_j / 2 pi (the turns of pair j over the
+ * trained length). */
+enum { MFMG_ROPE_PLAIN = 0, MFMG_ROPE_LINEAR = 1, MFMG_ROPE_BASE = 2, MFMG_ROPE_PARTS = 3 };
+
+typedef struct {
+  int heads, kv_heads;   /* 1 <= kv_heads <= heads <= 1024, heads a multiple of kv_heads */
+  int head_dim;          /* a multiple of 8 in [8, 128] */
+  int precision;         /* MFMG_PREC_* of the operands */
+  float scale;           /* of the scores; 0: 1 / sqrt(head_dim) */
+  int qk_norm;           /* 1: RMS norm x / sqrt(mean(x^2) + norm_eps) times a gain for every
+                            query and key head before the rotation */
+  float norm_eps;        /* > 0 with qk_norm */
+  int rope_dims;         /* the first rope_dims dims of a head rotate (even; 0: all) */
+  int rope_interleaved;  /* pairs (2j, 2j + 1) instead of (j, j + rope_dims / 2) */
+  float rope_base;       /* > 0 */
+  int rope_scaling;      /* MFMG_ROPE_* */
+  float rope_factor, rope_train_len, rope_slow, rope_fast;
+  float rope_mscale;     /* factor on the rotated dims; 0: 1 */
+} mfmg_attn_desc;
+
+typedef struct mfmg_attn* mfmg_attn_t;
+
+/* q, k and v rows of T with their leading dimensions (views of one QKV row matrix, or
+ * separate arrays). */
+typedef struct {
+  const void *q, *k, *v;
+  int64_t ldq, ldk, ldv;
+} mfmg_qkv;
+typedef struct {
+  void *q, *k, *v;
+  int64_t ldq, ldk, ldv;
+} mfmg_qkv_out;
+
+/* Validates `desc` and creates an immutable handle (host memory only; threads may
+ * share it). */
+mfmg_status mfmg_attn_create(const mfmg_attn_desc* desc, mfmg_attn_t* out);
+void mfmg_attn_destroy(mfmg_attn_t attn);
+
+/* Workspace bytes of mfmg_qk_rope_bwd and mfmg_attn_bwd for n_tokens rows. */
+mfmg_status mfmg_attn_ws_bytes(mfmg_attn_t attn, int64_t n_tokens, size_t* bytes);
+
+/* Device bytes of a plan over n_tokens rows (< 2^31 - 1024) and n_seqs sequences
+ * (<= 2^24). */
+mfmg_status mfmg_seq_plan_bytes(int64_t n_tokens, int n_seqs, size_t* bytes);
+
+/* Writes the plan of a batch into `plan` (dev, 256-byte aligned).  cu_seqlens (dev,
+ * n_seqs + 1 int32): sequence j is tokens cu_seqlens[j] .. cu_seqlens[j + 1] - 1
+ * (possibly none).  Offsets outside 0 .. n_tokens are clamped into it, and an offset
+ * below an earlier one counts as that one.  positions (dev, n_tokens int32, nullable):
+ * each token's rotary position; NULL: its index within its sequence.  The plan serves
+ * any number of calls with the same n_tokens and n_seqs, on any handles. */
+mfmg_status mfmg_seq_plan(const int32_t* cu_seqlens, int n_seqs, int64_t n_tokens,
+                          const int32_t* positions, void* plan, size_t plan_bytes, void* stream);
+
+/* Rotary positions on the query and key heads of QKV rows, after the norms with
+ * qk_norm; value heads are converted to T only.
+ *   x, xd (dev, float32 [n_tokens][ldx]), gain, gaind (dev, float32 [2][head_dim]: the
+ *   query heads' gain, then the key heads'; required with qk_norm, else NULL),
+ *   y, yd (dev, T [n_tokens][ldy]).  Outputs must not alias inputs. */
+mfmg_status mfmg_qk_rope_fwd(mfmg_attn_t attn, const void* plan, int64_t n_tokens, int n_seqs,
+                             const float* x, const float* xd, int64_t ldx, const float* gain,
+                             const float* gaind, void* y, void* yd, int64_t ldy, void* stream);
+
+/* Its backward: from dy (and its tangent dyd; T [n_tokens][lddy]) the gradient dx of x (T
+ * [n_tokens][lddx]) and with qk_norm dgain of the gains (float32 [2][head_dim]), and
+ * the derivatives dxd, dgaind of both along the tangents.  x, xd, gain, gaind as in the
+ * forward; x and xd only with qk_norm (else NULL).  ws: mfmg_attn_ws_bytes. */
+mfmg_status mfmg_qk_rope_bwd(mfmg_attn_t attn, const void* plan, int64_t n_tokens, int n_seqs,
+                             const float* x, const float* xd, int64_t ldx, const float* gain,
+                             const float* gaind, const void* dy, const void* dyd, int64_t lddy,
+                             void* dx, void* dxd, int64_t lddx, float* dgain, float* dgaind,
+                             void* ws, size_t ws_bytes, void* stream);
+
+/* Causal softmax attention of every sequence, o (dev, T [n_tokens][ldo]) and, with the
+ * tangents xd, od.  stats (dev, float32 [2][heads][n_tokens]): what the backward needs
+ * of every row (4-byte aligned). */
+mfmg_status mfmg_attn_fwd(mfmg_attn_t attn, const void* plan, int64_t n_tokens, int n_seqs,
+                          const mfmg_qkv* x, const mfmg_qkv* xd, void* o, void* od, int64_t ldo,
+                          float* stats, void* stream);
+
+/* Its backward: from g (dev, T [n_tokens][ldg]), the cotangent of o, the gradients dx of
+ * q, k and v (a key head's is the sum over the query heads that read it), and with the
+ * tangents xd, od, gd the derivatives dxd of those gradients along (xd, gd).  o, od,
+ * stats: of the forward with the same x (and xd).  ws: mfmg_attn_ws_bytes. */
+mfmg_status mfmg_attn_bwd(mfmg_attn_t attn, const void* plan, int64_t n_tokens, int n_seqs,
+                          const mfmg_qkv* x, const mfmg_qkv* xd, const void* o, const void* od,
+                          int64_t ldo, const float* stats, const void* g, const void* gd,
+                          int64_t ldg, const mfmg_qkv_out* dx, const mfmg_qkv_out* dxd, void* ws,
+                          size_t ws_bytes, void* stream);
+
 /* Non-finite check of a result, e.g. d_eta_out of mfmg_meta_grad (whose
  * calls never inspect their outputs: that would need a host synchronisation
  * inside the call).  Counts the NaN and infinite entries of x (dev, n floats)

@@ -4,4 +4,4 @@
 library in-tree.  Importing the package does not load the library.
 """
 from . import _lib  # noqa: F401
-from ._lib import Problem, make_desc, lib, MfmgError  # noqa: F401
+from ._lib import Attention, Problem, lib, make_attn_desc, make_desc, mfmg_seq_plan, MfmgError  # noqa: F401

@@ -21,7 +21,10 @@ EXPORTED = [
     "mfmg_problem_create", "mfmg_problem_destroy", "mfmg_query_sizes", "mfmg_inner_step",
     "mfmg_hvp_fwd_over_rev", "mfmg_meta_grad", "mfmg_status_string", "mfmg_last_error_message",
     "mfmg_timing_enable", "mfmg_timing_read", "mfmg_check_finite", "mfmg_meta_grad_noalloc",
+    "mfmg_attn_create", "mfmg_attn_destroy", "mfmg_attn_ws_bytes", "mfmg_seq_plan_bytes",
+    "mfmg_seq_plan", "mfmg_qk_rope_fwd", "mfmg_qk_rope_bwd", "mfmg_attn_fwd", "mfmg_attn_bwd",
 ]
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_PARTS = 0, 1, 2, 3
 NOALLOC_SCRATCH_BYTES = 64 * 1024 * 1024   # MFMG_NOALLOC_SCRATCH_BYTES
 
 
@@ -46,6 +49,19 @@ class mfmg_sizes(ctypes.Structure):
 
 class mfmg_batch(ctypes.Structure):
     _fields_ = [("x", c_void_p), ("y", c_void_p), ("rows", c_int64)]
+
+
+class mfmg_attn_desc(ctypes.Structure):
+    _fields_ = [("heads", c_int), ("kv_heads", c_int), ("head_dim", c_int), ("precision", c_int),
+                ("scale", c_float), ("qk_norm", c_int), ("norm_eps", c_float), ("rope_dims", c_int),
+                ("rope_interleaved", c_int), ("rope_base", c_float), ("rope_scaling", c_int),
+                ("rope_factor", c_float), ("rope_train_len", c_float), ("rope_slow", c_float),
+                ("rope_fast", c_float), ("rope_mscale", c_float)]
+
+
+class mfmg_qkv(ctypes.Structure):   # mfmg_qkv and mfmg_qkv_out
+    _fields_ = [("q", c_void_p), ("k", c_void_p), ("v", c_void_p),
+                ("ldq", c_int64), ("ldk", c_int64), ("ldv", c_int64)]
 
 
 class MfmgError(RuntimeError):
@@ -91,7 +107,24 @@ def lib() -> ctypes.CDLL:
     L.mfmg_last_error_message.restype = c_char_p
     L.mfmg_timing_enable.argtypes = [c_int]
     L.mfmg_timing_read.argtypes = [c_int, P(c_int), P(c_double)]
-    for name in ("mfmg_problem_create", "mfmg_query_sizes", "mfmg_inner_step",
+    L.mfmg_attn_create.argtypes = [P(mfmg_attn_desc), P(c_void_p)]
+    L.mfmg_attn_destroy.argtypes = [c_void_p]
+    L.mfmg_attn_destroy.restype = None
+    L.mfmg_attn_ws_bytes.argtypes = [c_void_p, c_int64, P(c_size_t)]
+    L.mfmg_seq_plan_bytes.argtypes = [c_int64, c_int, P(c_size_t)]
+    L.mfmg_seq_plan.argtypes = [c_void_p, c_int, c_int64, c_void_p, c_void_p, c_size_t, c_void_p]
+    rows = [c_void_p, c_void_p, c_int64]   # an array, its tangent, their leading dimension
+    head = [c_void_p, c_void_p, c_int64, c_int]   # handle, plan, n_tokens, n_seqs
+    ws = [c_void_p, c_size_t, c_void_p]   # workspace, its bytes, stream
+    L.mfmg_qk_rope_fwd.argtypes = head + rows + [c_void_p, c_void_p] + rows + [c_void_p]
+    L.mfmg_qk_rope_bwd.argtypes = (head + rows + [c_void_p, c_void_p] + rows + rows
+                                   + [c_void_p, c_void_p] + ws)
+    L.mfmg_attn_fwd.argtypes = head + [P(mfmg_qkv), P(mfmg_qkv)] + rows + [c_void_p, c_void_p]
+    L.mfmg_attn_bwd.argtypes = (head + [P(mfmg_qkv), P(mfmg_qkv)] + rows + [c_void_p] + rows
+                                + [P(mfmg_qkv), P(mfmg_qkv)] + ws)
+    for name in ("mfmg_attn_create", "mfmg_attn_ws_bytes", "mfmg_seq_plan_bytes", "mfmg_seq_plan",
+                 "mfmg_qk_rope_fwd", "mfmg_qk_rope_bwd", "mfmg_attn_fwd", "mfmg_attn_bwd",
+                 "mfmg_problem_create", "mfmg_query_sizes", "mfmg_inner_step",
                  "mfmg_hvp_fwd_over_rev", "mfmg_meta_grad", "mfmg_timing_enable",
                  "mfmg_timing_read", "mfmg_check_finite", "mfmg_meta_grad_noalloc"):
         getattr(L, name).restype = c_int
@@ -208,6 +241,186 @@ class Problem:
                                            arr, T, ctypes.byref(vb), _ptr(d_eta_out),
                                            _ptr(val_loss_out), ctypes.byref(peak), _stream()))
         return peak.value
+
+
+def make_attn_desc(*, heads, kv_heads=None, head_dim, precision=0, scale=0.0, qk_norm=False,
+                   norm_eps=1e-6, rope_dims=0, rope_interleaved=False, rope_base=10000.0,
+                   rope_scaling=ROPE_PLAIN, rope_factor=1.0, rope_train_len=0.0, rope_slow=1.0,
+                   rope_fast=32.0, rope_mscale=0.0) -> mfmg_attn_desc:
+    return mfmg_attn_desc(heads, heads if kv_heads is None else kv_heads, head_dim, precision, scale,
+                          int(bool(qk_norm)), norm_eps, rope_dims, int(bool(rope_interleaved)),
+                          rope_base, rope_scaling, rope_factor, rope_train_len, rope_slow, rope_fast,
+                          rope_mscale)
+
+
+def _bad(message: str):
+    return MfmgError(ERR_INVALID_ARGUMENT, f"MFMG_ERR_INVALID_ARGUMENT: {message}")
+
+
+def _check_dev(name, t, dtype):
+    """t is a tensor of dtype on the current device (None passes)."""
+    import torch
+    if t is None:
+        return
+    if t.dtype != dtype:
+        raise _bad(f"{name}: {t.dtype}, expected {dtype}")
+    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+        raise _bad(f"{name} is on {t.device}, expected the current device")
+
+
+class SeqPlan:
+    """The plan of a batch's sequences (mfmg_seq_plan): device memory with its sizes."""
+
+    def __init__(self, data, n_tokens: int, n_seqs: int):
+        self.data, self.n_tokens, self.n_seqs = data, n_tokens, n_seqs
+
+
+def mfmg_seq_plan(cu_seqlens, n_tokens: int, positions=None, plan=None) -> SeqPlan:
+    """Plan of n_tokens rows holding len(cu_seqlens) - 1 sequences; `plan` reuses the device
+    memory of an earlier one of the same sizes."""
+    import torch
+    _check_dev("cu_seqlens", cu_seqlens, torch.int32)
+    _check_dev("positions", positions, torch.int32)
+    m = cu_seqlens.numel() - 1
+    if m < 0 or not cu_seqlens.is_contiguous():
+        raise _bad("cu_seqlens must be contiguous with at least one entry")
+    if positions is not None and (positions.numel() != n_tokens or not positions.is_contiguous()):
+        raise _bad("positions must be contiguous, one per token")
+    if plan is None:
+        n = c_size_t(0)
+        check(lib().mfmg_seq_plan_bytes(n_tokens, m, ctypes.byref(n)))
+        plan = SeqPlan(torch.empty(n.value, dtype=torch.uint8, device=cu_seqlens.device), n_tokens, m)
+    elif (plan.n_tokens, plan.n_seqs) != (n_tokens, m):
+        raise _bad("the plan to reuse is of other sizes")
+    _check_dev("plan", plan.data, torch.uint8)
+    check(lib().mfmg_seq_plan(_ptr(cu_seqlens), m, n_tokens, _ptr(positions), _ptr(plan.data),
+                              plan.data.numel(), _stream()))
+    return plan
+
+
+class Attention:
+    """Owns an mfmg_attn_t handle.  Row arguments are 2-D tensors [n_tokens][columns] whose rows
+    are contiguous (views of wider rows pass); optional ones may be None as in the C calls."""
+
+    def __init__(self, desc: mfmg_attn_desc):
+        import torch
+        self._h = c_void_p()
+        check(lib().mfmg_attn_create(ctypes.byref(desc), ctypes.byref(self._h)))
+        self.desc = desc
+        self.dtype = torch.bfloat16 if desc.precision == 1 else torch.float32
+        self.q_cols = desc.heads * desc.head_dim
+        self.kv_cols = desc.kv_heads * desc.head_dim
+
+    def __del__(self):
+        h = getattr(self, "_h", None)
+        if h is not None and h.value and _lib is not None:
+            _lib.mfmg_attn_destroy(h)
+            self._h = c_void_p()
+
+    def mfmg_attn_ws_bytes(self, n_tokens: int) -> int:
+        n = c_size_t(0)
+        check(lib().mfmg_attn_ws_bytes(self._h, n_tokens, ctypes.byref(n)))
+        return n.value
+
+    def workspace(self, n_tokens: int, device="cuda"):
+        """A workspace of the backward calls (torch allocation)."""
+        import torch
+        return torch.empty(max(self.mfmg_attn_ws_bytes(n_tokens), 1), dtype=torch.uint8, device=device)
+
+    @staticmethod
+    def _rows(name, t, cols, dtype, n):
+        """The leading dimension of row tensor t (0: None)."""
+        if t is None:
+            return 0
+        _check_dev(name, t, dtype)
+        if t.dim() != 2 or t.shape[0] != n or t.shape[1] != cols:
+            raise _bad(f"{name}: shape {tuple(t.shape)}, expected ({n}, {cols})")
+        if n and t.stride(1) != 1:
+            raise _bad(f"{name}: rows are not contiguous")
+        return t.stride(0) if n > 1 else cols
+
+    def _pair(self, name, t, td, cols, dtype, n):
+        """The one leading dimension of an array and its tangent."""
+        ld = self._rows(name, t, cols, dtype, n)
+        ldd = self._rows(name + "d", td, cols, dtype, n)
+        if td is not None and t is not None and ld != ldd:
+            raise _bad(f"{name} and {name}d have different row strides")
+        return ld if t is not None else ldd
+
+    def _gains(self, *ts):
+        import torch
+        for name, t in zip(("gain", "gaind", "dgain", "dgaind"), ts):
+            if t is not None:
+                _check_dev(name, t, torch.float32)
+                if tuple(t.shape) != (2, self.desc.head_dim) or not t.is_contiguous():
+                    raise _bad(f"{name}: expected a contiguous (2, {self.desc.head_dim})")
+
+    def _qkv(self, name, q, k, v, n):
+        """mfmg_qkv of three row tensors; None if none is given."""
+        if q is None and k is None and v is None:
+            return None
+        if q is None or k is None or v is None:
+            raise _bad(f"{name}: q, k and v go together")
+        ld = [self._rows(f"{name}.{c}", t, w, self.dtype, n)
+              for c, t, w in (("q", q, self.q_cols), ("k", k, self.kv_cols), ("v", v, self.kv_cols))]
+        return ctypes.byref(mfmg_qkv(q.data_ptr(), k.data_ptr(), v.data_ptr(), *ld))
+
+    def _plan(self, plan, ws=None):
+        import torch
+        _check_dev("plan", plan.data, torch.uint8)
+        if ws is not None:
+            _check_dev("ws", ws, torch.uint8)
+        return self._h, _ptr(plan.data), plan.n_tokens, plan.n_seqs
+
+    def mfmg_qk_rope_fwd(self, plan, x, y, gain=None, xd=None, gaind=None, yd=None):
+        import torch
+        n, w = plan.n_tokens, self.q_cols + 2 * self.kv_cols
+        ldx = self._pair("x", x, xd, w, torch.float32, n)
+        ldy = self._pair("y", y, yd, w, self.dtype, n)
+        self._gains(gain, gaind)
+        check(lib().mfmg_qk_rope_fwd(*self._plan(plan), _ptr(x), _ptr(xd), ldx, _ptr(gain),
+                                     _ptr(gaind), _ptr(y), _ptr(yd), ldy, _stream()))
+
+    def mfmg_qk_rope_bwd(self, plan, dy, dx, x=None, gain=None, dgain=None, dyd=None, dxd=None,
+                         xd=None, gaind=None, dgaind=None, ws=None):
+        import torch
+        n, w = plan.n_tokens, self.q_cols + 2 * self.kv_cols
+        ldx = self._pair("x", x, xd, w, torch.float32, n)
+        lddy = self._pair("dy", dy, dyd, w, self.dtype, n)
+        lddx = self._pair("dx", dx, dxd, w, self.dtype, n)
+        self._gains(gain, gaind, dgain, dgaind)
+        if ws is None:
+            ws = self.workspace(n, dy.device)
+        check(lib().mfmg_qk_rope_bwd(*self._plan(plan, ws), _ptr(x), _ptr(xd), ldx, _ptr(gain),
+                                     _ptr(gaind), _ptr(dy), _ptr(dyd), lddy, _ptr(dx), _ptr(dxd), lddx,
+                                     _ptr(dgain), _ptr(dgaind), _ptr(ws), ws.numel(), _stream()))
+
+    def _stats(self, stats, n):
+        import torch
+        _check_dev("stats", stats, torch.float32)
+        if stats.numel() != 2 * self.desc.heads * n or not stats.is_contiguous():
+            raise _bad(f"stats: expected a contiguous (2, {self.desc.heads}, {n})")
+        return _ptr(stats)
+
+    def mfmg_attn_fwd(self, plan, q, k, v, o, stats, qd=None, kd=None, vd=None, od=None):
+        n = plan.n_tokens
+        ldo = self._pair("o", o, od, self.q_cols, self.dtype, n)
+        check(lib().mfmg_attn_fwd(*self._plan(plan), self._qkv("x", q, k, v, n),
+                                  self._qkv("xd", qd, kd, vd, n), _ptr(o), _ptr(od), ldo,
+                                  self._stats(stats, n), _stream()))
+
+    def mfmg_attn_bwd(self, plan, q, k, v, o, stats, g, dq, dk, dv, qd=None, kd=None, vd=None,
+                      od=None, dod=None, dqd=None, dkd=None, dvd=None, ws=None):
+        n = plan.n_tokens
+        ldo = self._pair("o", o, od, self.q_cols, self.dtype, n)
+        ldg = self._pair("g", g, dod, self.q_cols, self.dtype, n)
+        if ws is None:
+            ws = self.workspace(n, o.device)
+        check(lib().mfmg_attn_bwd(*self._plan(plan, ws), self._qkv("x", q, k, v, n),
+                                  self._qkv("xd", qd, kd, vd, n), _ptr(o), _ptr(od), ldo,
+                                  self._stats(stats, n), _ptr(g), _ptr(dod), ldg,
+                                  self._qkv("dx", dq, dk, dv, n), self._qkv("dxd", dqd, dkd, dvd, n),
+                                  _ptr(ws), ws.numel(), _stream()))
 
 
 def mfmg_check_finite(x, ws=None) -> int:

@@ -28,6 +28,7 @@
 
 #include "kernels.h"
 #include "mfmg.h"
+#include "packed.h"
 #include "tf_engine.h"
 
 using namespace mfmg;
@@ -908,6 +909,86 @@ mfmg_status check_ws(void* ws, size_t ws_bytes, size_t need) {
 }  // namespace
 
 // ------------------------------------------------------------------------------------
+// Attention operators: handle and host-side checks
+// ------------------------------------------------------------------------------------
+struct mfmg_attn {
+  mfmg_attn_desc d;
+  RopeFreqs freqs;
+  int64_t width() const { return (int64_t)(d.heads + 2 * d.kv_heads) * d.head_dim; }
+  int size() const { return d.precision == MFMG_PREC_BF16 ? 2 : 4; }
+  float scale() const { return d.scale != 0.f ? d.scale : 1.0f / std::sqrt((float)d.head_dim); }
+};
+
+namespace {
+
+mfmg_status check_tokens(int64_t n, int m) {
+  if (n < 0 || n > PK_MAX_TOKENS)
+    return fail(MFMG_ERR_INVALID_ARGUMENT, "n_tokens %lld outside [0, 2^31 - 1024]", (long long)n);
+  if (m < 0 || m > PK_MAX_SEQS)
+    return fail(MFMG_ERR_INVALID_ARGUMENT, "n_seqs %d outside [0, 2^24]", m);
+  return MFMG_OK;
+}
+
+mfmg_status check_plan(const void* plan) {
+  if (!plan) return fail(MFMG_ERR_INVALID_ARGUMENT, "null plan");
+  if (!aligned(plan, 256)) return fail(MFMG_ERR_INVALID_ARGUMENT, "plan not 256-byte aligned");
+  return MFMG_OK;
+}
+
+mfmg_status check_attn(const mfmg_attn* a, const void* plan, int64_t n, int m) {
+  if (!a) return fail(MFMG_ERR_INVALID_ARGUMENT, "null attn");
+  TRY(check_tokens(n, m));
+  return check_plan(plan);
+}
+
+// A row matrix of `cols` columns of elements of `size` bytes.
+mfmg_status check_rows(const char* name, const void* p, int64_t ld, int64_t cols, int size) {
+  if (!p) return fail(MFMG_ERR_INVALID_ARGUMENT, "null %s", name);
+  if (!aligned(p, 16)) return fail(MFMG_ERR_INVALID_ARGUMENT, "%s not 16-byte aligned", name);
+  if (ld < cols || ld > (1LL << 31) || ld * size % 16)
+    return fail(MFMG_ERR_INVALID_ARGUMENT,
+                "%s: leading dimension %lld, needs at least %lld and rows of whole 16 bytes", name,
+                (long long)ld, (long long)cols);
+  return MFMG_OK;
+}
+
+mfmg_status check_gains(const mfmg_attn* a, const float* gain, const float* gaind, bool dual) {
+  if (!a->d.qk_norm) {
+    if (gain || gaind)
+      return fail(MFMG_ERR_INVALID_ARGUMENT, "gain and gaind must be NULL without qk_norm");
+    return MFMG_OK;
+  }
+  if (!gain || (dual && !gaind)) return fail(MFMG_ERR_INVALID_ARGUMENT, "null gain or gaind");
+  return check_align16({gain, gaind});
+}
+
+size_t attn_ws_bytes(const mfmg_attn* a, int64_t n) {
+  size_t w = 8 * (size_t)a->d.heads * (size_t)n;   // r and rd of the attention backward
+  if (a->d.qk_norm && n > 0)
+    w = std::max(w, 16 * (size_t)a->d.head_dim *
+                        (size_t)qk_rope_parts(n, a->d.heads, a->d.kv_heads, a->d.head_dim));
+  return (size_t)rup((long)w, 256);
+}
+
+template <typename T>
+QkRopeArgs<T> rope_args(const mfmg_attn* a, const void* plan, int64_t n, int m, const float* x,
+                        const float* xd, int64_t ldx, const float* gain, const float* gaind,
+                        bool dual) {
+  QkRopeArgs<T> r;
+  std::memset(&r, 0, sizeof(r));
+  r.x = x; r.xd = xd; r.ldx = r.ldxd = ldx;
+  r.gain = gain; r.gaind = gaind;
+  r.p = seq_plan_at((char*)plan, n, m, nullptr);
+  r.H = a->d.heads; r.K = a->d.kv_heads; r.dh = a->d.head_dim;
+  r.dual = dual;
+  r.eps = a->d.norm_eps;
+  r.f = a->freqs;
+  return r;
+}
+
+}  // namespace
+
+// ------------------------------------------------------------------------------------
 // Kernel timing
 // ------------------------------------------------------------------------------------
 namespace mfmg {
@@ -1290,6 +1371,264 @@ mfmg_status mfmg_meta_grad_noalloc(mfmg_problem_t p, const float* theta0,
   TRY(scratch_of_current_device(&ws));
   return meta_grad_run(p, theta0, opt_state0, eta, train_batches, T, val_batch, d_eta_out,
                        val_loss_out, peak_bytes_out, need, ws, stream);
+}
+
+// ------------------------------------------------------------------------------------
+// Attention operators
+// ------------------------------------------------------------------------------------
+mfmg_status mfmg_attn_create(const mfmg_attn_desc* desc, mfmg_attn_t* out) {
+  if (!desc || !out) return fail(MFMG_ERR_INVALID_ARGUMENT, "null desc or out");
+  *out = nullptr;
+  if (const char* msg = attn_desc_error(*desc)) return fail(MFMG_ERR_INVALID_ARGUMENT, "%s", msg);
+  mfmg_attn* a = new (std::nothrow) mfmg_attn;
+  if (!a) return fail(MFMG_ERR_INVALID_ARGUMENT, "out of host memory");
+  a->d = *desc;
+  a->freqs = rope_freqs(*desc);
+  *out = a;
+  return MFMG_OK;
+}
+
+void mfmg_attn_destroy(mfmg_attn_t a) { delete a; }
+
+mfmg_status mfmg_attn_ws_bytes(mfmg_attn_t a, int64_t n, size_t* bytes) {
+  if (!a || !bytes) return fail(MFMG_ERR_INVALID_ARGUMENT, "null attn or bytes");
+  TRY(check_tokens(n, 0));
+  *bytes = attn_ws_bytes(a, n);
+  return MFMG_OK;
+}
+
+mfmg_status mfmg_seq_plan_bytes(int64_t n, int m, size_t* bytes) {
+  if (!bytes) return fail(MFMG_ERR_INVALID_ARGUMENT, "null bytes");
+  TRY(check_tokens(n, m));
+  seq_plan_at(nullptr, n, m, bytes);
+  return MFMG_OK;
+}
+
+mfmg_status mfmg_seq_plan(const int32_t* cu, int m, int64_t n, const int32_t* positions, void* plan,
+                          size_t plan_bytes, void* stream) {
+  TRY(check_tokens(n, m));
+  if (!cu) return fail(MFMG_ERR_INVALID_ARGUMENT, "null cu_seqlens");
+  if (!aligned(cu, 4) || !aligned(positions, 4))
+    return fail(MFMG_ERR_INVALID_ARGUMENT, "cu_seqlens and positions must be 4-byte aligned");
+  size_t need = 0;
+  SeqPlanArgs a;
+  a.p = seq_plan_at(static_cast<char*>(plan), n, m, &need);
+  if (plan_bytes < need)
+    return fail(MFMG_ERR_WORKSPACE, "plan of %zu bytes, %zu required", plan_bytes, need);
+  TRY(check_plan(plan));
+  a.cu = cu;
+  a.positions = positions;
+  a.cover = 0;
+  a.len = 0;
+  HIPCHK(seq_plan_make(a, static_cast<hipStream_t>(stream)));
+  return MFMG_OK;
+}
+
+mfmg_status mfmg_qk_rope_fwd(mfmg_attn_t a, const void* plan, int64_t n, int m, const float* x,
+                             const float* xd, int64_t ldx, const float* gain, const float* gaind,
+                             void* y, void* yd, int64_t ldy, void* stream) {
+  TRY(check_attn(a, plan, n, m));
+  const int64_t W = a->width();
+  const bool dual = xd || yd || gaind;
+  if (n > 0 && dual && (!xd || !yd || (a->d.qk_norm && !gaind)))
+    return fail(MFMG_ERR_INVALID_ARGUMENT, "the tangents xd, yd and (with qk_norm) gaind go together");
+  TRY(check_gains(a, gain, gaind, dual));
+  if (n == 0) return MFMG_OK;
+  TRY(check_rows("x", x, ldx, W, 4));
+  TRY(check_rows("y", y, ldy, W, a->size()));
+  if (dual) {
+    TRY(check_rows("xd", xd, ldx, W, 4));
+    TRY(check_rows("yd", yd, ldy, W, a->size()));
+  }
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (a->d.precision == MFMG_PREC_BF16) {
+    QkRopeArgs<bf16_t> r = rope_args<bf16_t>(a, plan, n, m, x, xd, ldx, gain, gaind, dual);
+    r.y = (bf16_t*)y; r.yd = (bf16_t*)yd; r.ldy = r.ldyd = ldy;
+    HIPCHK(qk_rope_fwd(r, s));
+  } else {
+    QkRopeArgs<float> r = rope_args<float>(a, plan, n, m, x, xd, ldx, gain, gaind, dual);
+    r.y = (float*)y; r.yd = (float*)yd; r.ldy = r.ldyd = ldy;
+    HIPCHK(qk_rope_fwd(r, s));
+  }
+  return MFMG_OK;
+}
+
+}  // extern "C"
+
+namespace {
+template <typename T>
+mfmg_status run_rope_bwd(QkRopeArgs<T> r, const void* dy, const void* dyd, int64_t lddy, void* dx,
+                         void* dxd, int64_t lddx, float* dgain, float* dgaind, void* ws,
+                         hipStream_t s) {
+  r.y = (T*)dy; r.yd = (T*)dyd; r.ldy = r.ldyd = lddy;   // (read only in the backward)
+  r.dx = (T*)dx; r.dxd = (T*)dxd; r.lddx = r.lddxd = lddx;
+  r.partial = static_cast<float*>(ws);
+  HIPCHK(qk_rope_bwd(r, s));
+  if (r.gain && r.p.n > 0) {
+    ParamArgs<T> P;
+    std::memset(&P, 0, sizeof(P));
+    P.mode = r.dual ? P_HVP : P_STORE_G;
+    P.grad_out = dgain;
+    P.hvp_out = dgaind;
+    HIPCHK(gain_param<T>(r.partial, qk_rope_parts(r.p.n, r.H, r.K, r.dh), r.dh, 0, r.dh, P, nullptr,
+                         nullptr, s));
+  } else if (r.gain) {
+    HIPCHK(fill(dgain, 2 * r.dh, 0.f, s));
+    if (r.dual) HIPCHK(fill(dgaind, 2 * r.dh, 0.f, s));
+  }
+  return MFMG_OK;
+}
+
+template <typename T>
+PackedAttnArgs<T> packed_args(const mfmg_attn* a, const void* plan, int64_t n, int m,
+                              const mfmg_qkv* x, const mfmg_qkv* xd) {
+  PackedAttnArgs<T> p;
+  std::memset(&p, 0, sizeof(p));
+  p.q = (const T*)x->q; p.k = (const T*)x->k; p.v = (const T*)x->v;
+  p.ldq = x->ldq; p.ldk = x->ldk; p.ldv = x->ldv;
+  if (xd) {
+    p.qd = (const T*)xd->q; p.kd = (const T*)xd->k; p.vd = (const T*)xd->v;
+    p.ldqd = xd->ldq; p.ldkd = xd->ldk; p.ldvd = xd->ldv;
+  }
+  p.p = seq_plan_at((char*)plan, n, m, nullptr);
+  p.H = a->d.heads; p.K = a->d.kv_heads; p.dh = a->d.head_dim;
+  p.dual = xd != nullptr;
+  p.scale = a->scale();
+  return p;
+}
+
+template <typename T>
+mfmg_status run_attn_fwd(PackedAttnArgs<T> p, void* o, void* od, int64_t ldo, float* stats,
+                         hipStream_t s) {
+  p.o = (T*)o; p.od = (T*)od; p.ldo = p.ldod = ldo;
+  p.lse = stats; p.cst = stats + (long)p.H * p.p.n;
+  HIPCHK(packed_attn_fwd(p, s));
+  return MFMG_OK;
+}
+
+template <typename T>
+mfmg_status run_attn_bwd(PackedAttnArgs<T> p, const void* o, const void* od, int64_t ldo,
+                         const float* stats, const void* g, const void* gd, int64_t ldg,
+                         const mfmg_qkv_out* dx, const mfmg_qkv_out* dxd, void* ws, hipStream_t s) {
+  p.o = (T*)o; p.od = (T*)od; p.ldo = p.ldod = ldo;   // (read only in the backward)
+  p.lse = (float*)stats; p.cst = (float*)stats + (long)p.H * p.p.n;
+  p.g = (const T*)g; p.gd = (const T*)gd; p.ldg = p.ldgd = ldg;
+  p.dq = (T*)dx->q; p.dk = (T*)dx->k; p.dv = (T*)dx->v;
+  p.lddq = dx->ldq; p.lddk = dx->ldk; p.lddv = dx->ldv;
+  if (dxd) {
+    p.dqd = (T*)dxd->q; p.dkd = (T*)dxd->k; p.dvd = (T*)dxd->v;
+    p.lddqd = dxd->ldq; p.lddkd = dxd->ldk; p.lddvd = dxd->ldv;
+  }
+  p.r = static_cast<float*>(ws);
+  p.rd = p.r + (long)p.H * p.p.n;
+  HIPCHK(packed_attn_bwd(p, s));
+  return MFMG_OK;
+}
+
+mfmg_status check_qkv(const mfmg_attn* a, const char* name, const void* q, const void* k,
+                      const void* v, int64_t ldq, int64_t ldk, int64_t ldv) {
+  const int64_t qw = (int64_t)a->d.heads * a->d.head_dim, kw = (int64_t)a->d.kv_heads * a->d.head_dim;
+  char what[16];
+  snprintf(what, sizeof(what), "%s.q", name);
+  TRY(check_rows(what, q, ldq, qw, a->size()));
+  snprintf(what, sizeof(what), "%s.k", name);
+  TRY(check_rows(what, k, ldk, kw, a->size()));
+  snprintf(what, sizeof(what), "%s.v", name);
+  return check_rows(what, v, ldv, kw, a->size());
+}
+}  // namespace
+
+extern "C" {
+
+mfmg_status mfmg_qk_rope_bwd(mfmg_attn_t a, const void* plan, int64_t n, int m, const float* x,
+                             const float* xd, int64_t ldx, const float* gain, const float* gaind,
+                             const void* dy, const void* dyd, int64_t lddy, void* dx, void* dxd,
+                             int64_t lddx, float* dgain, float* dgaind, void* ws, size_t ws_bytes,
+                             void* stream) {
+  TRY(check_attn(a, plan, n, m));
+  const int64_t W = a->width();
+  const bool dual = dyd || dxd || xd || gaind || dgaind, norm = a->d.qk_norm;
+  // (arrays of no rows may be NULL)
+  if (dual && ((n > 0 && (!dyd || !dxd || (norm && !xd))) || (norm && (!gaind || !dgaind))))
+    return fail(MFMG_ERR_INVALID_ARGUMENT,
+                "the tangents dyd, dxd and (with qk_norm) xd, gaind, dgaind go together");
+  TRY(check_gains(a, gain, gaind, dual));
+  if (norm) {
+    if (!dgain) return fail(MFMG_ERR_INVALID_ARGUMENT, "null dgain");
+    TRY(check_align16({dgain, dgaind}));
+    if (n > 0) TRY(check_rows("x", x, ldx, W, 4));
+    if (n > 0 && dual) TRY(check_rows("xd", xd, ldx, W, 4));
+  } else if (x || xd || dgain || dgaind) {
+    return fail(MFMG_ERR_INVALID_ARGUMENT, "x, xd, dgain and dgaind must be NULL without qk_norm");
+  }
+  if (n > 0) {
+    TRY(check_rows("dy", dy, lddy, W, a->size()));
+    TRY(check_rows("dx", dx, lddx, W, a->size()));
+    if (dual) {
+      TRY(check_rows("dyd", dyd, lddy, W, a->size()));
+      TRY(check_rows("dxd", dxd, lddx, W, a->size()));
+    }
+  }
+  TRY(check_ws(ws, ws_bytes, attn_ws_bytes(a, n)));
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (a->d.precision == MFMG_PREC_BF16)
+    return run_rope_bwd(rope_args<bf16_t>(a, plan, n, m, x, xd, ldx, gain, gaind, dual), dy, dyd,
+                        lddy, dx, dxd, lddx, dgain, dgaind, ws, s);
+  return run_rope_bwd(rope_args<float>(a, plan, n, m, x, xd, ldx, gain, gaind, dual), dy, dyd, lddy,
+                      dx, dxd, lddx, dgain, dgaind, ws, s);
+}
+
+mfmg_status mfmg_attn_fwd(mfmg_attn_t a, const void* plan, int64_t n, int m, const mfmg_qkv* x,
+                          const mfmg_qkv* xd, void* o, void* od, int64_t ldo, float* stats,
+                          void* stream) {
+  TRY(check_attn(a, plan, n, m));
+  if (!x) return fail(MFMG_ERR_INVALID_ARGUMENT, "null x");
+  if (!xd != !od) return fail(MFMG_ERR_INVALID_ARGUMENT, "the tangents xd and od go together");
+  if (n == 0) return MFMG_OK;
+  const int64_t qw = (int64_t)a->d.heads * a->d.head_dim;
+  TRY(check_qkv(a, "x", x->q, x->k, x->v, x->ldq, x->ldk, x->ldv));
+  TRY(check_rows("o", o, ldo, qw, a->size()));
+  if (xd) {
+    TRY(check_qkv(a, "xd", xd->q, xd->k, xd->v, xd->ldq, xd->ldk, xd->ldv));
+    TRY(check_rows("od", od, ldo, qw, a->size()));
+  }
+  if (!stats || !aligned(stats, 4)) return fail(MFMG_ERR_INVALID_ARGUMENT, "null or misaligned stats");
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (a->d.precision == MFMG_PREC_BF16)
+    return run_attn_fwd(packed_args<bf16_t>(a, plan, n, m, x, xd), o, od, ldo, stats, s);
+  return run_attn_fwd(packed_args<float>(a, plan, n, m, x, xd), o, od, ldo, stats, s);
+}
+
+mfmg_status mfmg_attn_bwd(mfmg_attn_t a, const void* plan, int64_t n, int m, const mfmg_qkv* x,
+                          const mfmg_qkv* xd, const void* o, const void* od, int64_t ldo,
+                          const float* stats, const void* g, const void* gd, int64_t ldg,
+                          const mfmg_qkv_out* dx, const mfmg_qkv_out* dxd, void* ws,
+                          size_t ws_bytes, void* stream) {
+  TRY(check_attn(a, plan, n, m));
+  if (!x || !dx) return fail(MFMG_ERR_INVALID_ARGUMENT, "null x or dx");
+  const bool dual = xd || od || gd || dxd;
+  if (dual && !(xd && od && gd && dxd))
+    return fail(MFMG_ERR_INVALID_ARGUMENT, "the tangents xd, od, gd and dxd go together");
+  if (n == 0) return MFMG_OK;
+  const int64_t qw = (int64_t)a->d.heads * a->d.head_dim;
+  TRY(check_qkv(a, "x", x->q, x->k, x->v, x->ldq, x->ldk, x->ldv));
+  TRY(check_qkv(a, "dx", dx->q, dx->k, dx->v, dx->ldq, dx->ldk, dx->ldv));
+  TRY(check_rows("o", o, ldo, qw, a->size()));
+  TRY(check_rows("g", g, ldg, qw, a->size()));
+  if (dual) {
+    TRY(check_qkv(a, "xd", xd->q, xd->k, xd->v, xd->ldq, xd->ldk, xd->ldv));
+    TRY(check_qkv(a, "dxd", dxd->q, dxd->k, dxd->v, dxd->ldq, dxd->ldk, dxd->ldv));
+    TRY(check_rows("od", od, ldo, qw, a->size()));
+    TRY(check_rows("gd", gd, ldg, qw, a->size()));
+  }
+  if (!stats || !aligned(stats, 4)) return fail(MFMG_ERR_INVALID_ARGUMENT, "null or misaligned stats");
+  TRY(check_ws(ws, ws_bytes, attn_ws_bytes(a, n)));
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (a->d.precision == MFMG_PREC_BF16)
+    return run_attn_bwd(packed_args<bf16_t>(a, plan, n, m, x, xd), o, od, ldo, stats, g, gd, ldg, dx,
+                        dxd, ws, s);
+  return run_attn_bwd(packed_args<float>(a, plan, n, m, x, xd), o, od, ldo, stats, g, gd, ldg, dx,
+                      dxd, ws, s);
 }
 
 mfmg_status mfmg_check_finite(const float* x, size_t n, size_t* count_out, void* ws,

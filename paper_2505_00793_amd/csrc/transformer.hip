@@ -9,6 +9,7 @@
 // attention scores/probabilities float32 [batch * heads][seq][seq].
 #include "kernels.h"
 #include "param_epi.h"
+#include "packed.h"
 #include "transformer.h"
 
 namespace mfmg {
@@ -756,6 +757,14 @@ hipError_t ln_bwd(const LnBwdArgs& a, long g_off, long b_off, const ParamArgs<T>
   return hipGetLastError();
 }
 
+template <typename T>
+hipError_t gain_param(const float* partial, int parts, int d, long off0, long off1,
+                      const ParamArgs<T>& P, float* out0, float* out1, hipStream_t s) {
+  hipLaunchKernelGGL(ln_param_kernel<T>, dim3(cdivl(d, 16)), dim3(256), 0, s, partial, parts, d,
+                     off0, off1, P, out0, out1);
+  return hipGetLastError();
+}
+
 hipError_t rope_table(int S, int dh, double base, float* cs, float* sn, hipStream_t s) {
   hipLaunchKernelGGL(rope_table_kernel, dim3(cdivl((long)S * dh / 2, 256)), dim3(256), 0, s, S, dh,
                      base, cs, sn);
@@ -831,6 +840,8 @@ hipError_t meta_vjp(const float* hid, const float* ubar, int rows, int hdim, con
 
 template hipError_t ln_bwd<bf16_t>(const LnBwdArgs&, long, long, const ParamArgs<bf16_t>&, float*, float*, hipStream_t);
 template hipError_t ln_bwd<float>(const LnBwdArgs&, long, long, const ParamArgs<float>&, float*, float*, hipStream_t);
+template hipError_t gain_param<bf16_t>(const float*, int, int, long, long, const ParamArgs<bf16_t>&, float*, float*, hipStream_t);
+template hipError_t gain_param<float>(const float*, int, int, long, long, const ParamArgs<float>&, float*, float*, hipStream_t);
 template hipError_t embed_grad<bf16_t>(const EmbedGradArgs&, const ParamArgs<bf16_t>&, hipStream_t);
 template hipError_t embed_grad<float>(const EmbedGradArgs&, const ParamArgs<float>&, hipStream_t);
 

@@ -1,0 +1,218 @@
+"""Causal attention over packed sequences with grouped heads (mfmg_attn_fwd / mfmg_attn_bwd), primal
+and dual, against its float64 form within elementwise bounds (packed_ref.py): lengths from none to
+several tiles, head sizes that no tile has, strided rows, unused rows and sequences that hold NaN."""
+import math
+
+import pytest
+import torch
+
+import packed_ref as R
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2505_00793_amd import _lib
+    _lib.lib()
+
+
+def _lib():
+    from paper_2505_00793_amd import _lib as M
+    return M
+
+
+class Call:
+    """Inputs, buffers and handle of one batch: `before` unused rows, the sequences, `after` more."""
+
+    def __init__(self, prec, H, K, dh, lens, dual, before=0, after=0, seed=0, gap=0, scale=0.0):
+        M = _lib()
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        self.T = torch.bfloat16 if prec else torch.float32
+        self.n = n = before + sum(lens) + after
+        self.H, self.K, self.dh, self.lens, self.first, self.dual = H, K, dh, lens, before, dual
+        self.scale = scale or 1 / math.sqrt(dh)
+        self.op = M.Attention(M.make_attn_desc(heads=H, kv_heads=K, head_dim=dh, precision=prec, scale=scale))
+        cu = torch.tensor([before] + [before + sum(lens[:i + 1]) for i in range(len(lens))], dtype=torch.int32)
+        self.cu = cu.cuda()
+        self.plan = M.mfmg_seq_plan(self.cu, n)
+
+        def rows(w, s):
+            t = torch.randn(n, w + gap, device="cuda", generator=g).mul_(s).to(self.T)[:, :w]
+            t[:before] = float("nan")
+            t[n - after:] = float("nan")
+            return t
+        W = (H + 2 * K) * dh
+        cut = (H * dh, K * dh, K * dh)
+        self.x = rows(W, 1.2).split(cut, 1)
+        self.xd = rows(W, 0.4).split(cut, 1) if dual else (None,) * 3
+        self.g, self.gd = rows(H * dh, 1.0), rows(H * dh, 0.4) if dual else None
+        self.fill = 7.0
+
+        def out(w):
+            return torch.full((n, w + gap), self.fill, device="cuda", dtype=self.T)[:, :w]
+        self.o, self.od = out(H * dh), out(H * dh) if dual else None
+        self.dx = out(W).split(cut, 1)
+        self.dxd = out(W).split(cut, 1) if dual else (None,) * 3
+        self.stats = torch.full((2, H, n), float("nan"), device="cuda")
+        self.ws = self.op.workspace(n).fill_(255)
+
+    def run(self):
+        self.op.mfmg_attn_fwd(self.plan, *self.x, self.o, self.stats, *self.xd, self.od)
+        self.op.mfmg_attn_bwd(self.plan, *self.x, self.o, self.stats, self.g, *self.dx, *self.xd, self.od,
+                              self.gd, *self.dxd, ws=self.ws)
+        return self
+
+    def outputs(self):
+        d = {"o": self.o, "dq": self.dx[0], "dk": self.dx[1], "dv": self.dx[2]}
+        if self.dual:
+            d.update(od=self.od, dqd=self.dxd[0], dkd=self.dxd[1], dvd=self.dxd[2])
+        return d
+
+    def reference(self):
+        def v(t):
+            t = t.double().view(self.n, -1, self.dh) if t.is_contiguous() else t.double().reshape(self.n, -1, self.dh)
+            return torch.nan_to_num(t, nan=0.0, posinf=0.0, neginf=0.0)
+        return R.attention(*map(v, self.x), self.lens, self.scale, self.T,
+                           tan=tuple(map(v, self.xd)) if self.dual else None, g=v(self.g),
+                           gd=v(self.gd) if self.dual else None, first=self.first)
+
+    def check(self, skip=()):
+        """Every output within its bound (sequences in `skip` excepted), unused rows untouched."""
+        ref = self.reference()
+        used = torch.zeros(self.n, dtype=torch.bool, device="cuda")
+        lo = self.first
+        for i, L in enumerate(self.lens):
+            if i not in skip:
+                used[lo:lo + L] = True
+            lo += L
+        for name, got in self.outputs().items():
+            val, bound = (t.reshape(self.n, -1) for t in ref[name])
+            err = (got.double() - val).abs()[used]
+            worst = float((err / (bound[used] + 1e-30)).max()) if err.numel() else 0.0
+            assert worst <= 1.0, f"{name}: {worst:.2f} of its bound (or not a number)"
+            rest = torch.cat((got[:self.first], got[lo:]))
+            assert torch.equal(rest, torch.full_like(rest, self.fill)), f"{name}: unused rows were written"
+
+
+SHAPES = [
+    # heads, key heads, head size, lengths
+    (1, 1, 8, [1]),
+    (2, 1, 16, [1, 0, 2, 31, 32, 33]),
+    (4, 2, 64, [63, 64, 65, 1, 127]),
+    (3, 3, 40, [128, 129, 0, 0, 17]),
+    (8, 1, 128, [200, 5, 130]),
+    (6, 3, 72, [257, 300]),
+    (2, 2, 96, [64, 191]),
+    (4, 4, 64, [700]),
+    (2, 1, 128, [513]),
+]
+
+
+@pytest.mark.parametrize("dual", [False, True], ids=["primal", "dual"])
+@pytest.mark.parametrize("prec", [0, 1], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("H,K,dh,lens", SHAPES, ids=lambda v: str(v).replace(" ", ""))
+def test_against_float64(prec, dual, H, K, dh, lens):
+    print(f"\n[packed] H {H} K {K} dh {dh} lens {lens} prec {prec} dual {dual}", flush=True)
+    c = Call(prec, H, K, dh, lens, dual, before=3, after=70, gap=16).run()
+    torch.cuda.synchronize()
+    c.check()
+
+
+@pytest.mark.parametrize("prec", [0, 1], ids=["fp32", "bf16"])
+def test_many_short_sequences(prec):
+    lens = [1 + (7 * i) % 13 for i in range(90)] + [0] * 5 + [150]
+    print(f"\n[packed] {len(lens)} short sequences", flush=True)
+    c = Call(prec, 4, 2, 32, lens, True, after=1, scale=0.3).run()
+    torch.cuda.synchronize()
+    c.check()
+
+
+@pytest.mark.parametrize("prec", [0, 1], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")], ids=["nan", "inf"])
+def test_a_bad_sequence_stays_alone(prec, bad):
+    """A sequence whose rows are not finite changes nothing of its neighbours, bit for bit."""
+    lens = [70, 30, 140]
+    print(f"\n[packed] a sequence of {bad}", flush=True)
+    good = Call(prec, 2, 1, 64, lens, True).run()
+    c = Call(prec, 2, 1, 64, lens, True)
+    for t in (*c.x, *c.xd, c.g, c.gd):
+        t[70:100] = bad
+    c.run()
+    torch.cuda.synchronize()
+    for name, got in c.outputs().items():
+        want = good.outputs()[name]
+        assert torch.equal(got[:70], want[:70]) and torch.equal(got[100:], want[100:]), name
+
+
+@pytest.mark.parametrize("prec", [0, 1], ids=["fp32", "bf16"])
+def test_large_scores(prec):
+    """Scores of hundreds: one key takes all of a row, the maximum is subtracted before exp."""
+    print("\n[packed] large scores", flush=True)
+    c = Call(prec, 2, 2, 64, [90, 200], False, scale=8.0).run()
+    torch.cuda.synchronize()
+    o = c.o.float()
+    assert torch.isfinite(o).all()
+    q, k, v = (t.double().reshape(c.n, 2, 64) for t in c.x)
+    for lo, hi in ((0, 90), (90, 290)):
+        S = 8.0 * torch.einsum("qhd,khd->hqk", q[lo:hi], k[lo:hi])
+        S = S.masked_fill(torch.ones(hi - lo, hi - lo, device="cuda").triu(1).bool(), -math.inf)
+        top = S.topk(2, -1).values
+        sure = (top[..., 0] - top[..., 1] > 30) | (top[..., 1] == -math.inf)   # e^-30 of the rest
+        pick = torch.stack([v[lo:hi, h][S[h].argmax(-1)] for h in range(2)])
+        got = c.o[lo:hi].double().reshape(hi - lo, 2, 64).transpose(0, 1)
+        assert sure.any()
+        # weights 1 to within e^-30 and the denominator's float32 steps: v itself, rounded once
+        assert (got - pick).abs()[sure].max() <= 1e-5
+
+
+def test_calls_repeat_bit_for_bit_and_in_graphs():
+    """Two plans on one stream, replays of a captured call and a call on another stream all give the
+    eager result."""
+    M = _lib()
+    print("\n[packed] graph and streams", flush=True)
+    c = Call(1, 4, 2, 64, [100, 37, 260], True, after=5).run()
+    want = {k: t.clone() for k, t in c.outputs().items()}
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        c.run()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(t, want[k]) for k, t in c.outputs().items())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        M.mfmg_seq_plan(c.cu, c.n, plan=c.plan)
+        c.run()
+    other = Call(1, 2, 2, 128, [64, 500], False, seed=3)
+    for k in range(3):
+        for t in c.outputs().values():
+            t.fill_(c.fill)
+        graph.replay()
+        other.run()
+        torch.cuda.synchronize()
+        assert all(torch.equal(t, want[n]) for n, t in c.outputs().items()), f"replay {k}"
+    other.check()
+
+
+def test_long_rows_pass_32_bit_offsets():
+    """Rows 2^20 elements apart, so that the last ones lie past 2^31 elements."""
+    print("\n[packed] wide rows", flush=True)
+    M = _lib()
+    n, H, dh, ld = 2200, 2, 64, 1 << 20
+    op = M.Attention(M.make_attn_desc(heads=H, kv_heads=1, head_dim=dh, precision=1))
+    big = torch.empty(n, ld, device="cuda", dtype=torch.bfloat16)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    W = (H + 2) * dh
+    x = torch.randn(n, W, device="cuda", generator=g).bfloat16()
+    big[:, :W] = x
+    plan = M.mfmg_seq_plan(torch.tensor([0, 1000, n], dtype=torch.int32, device="cuda"), n)
+    stats = torch.empty(2, H, n, device="cuda")
+    cut = (H * dh, dh, dh)
+    o, o2 = big[:, 1024:1024 + H * dh], torch.empty(n, H * dh, device="cuda", dtype=torch.bfloat16)
+    op.mfmg_attn_fwd(plan, *big[:, :W].split(cut, 1), o, stats)
+    op.mfmg_attn_fwd(plan, *x.split(cut, 1), o2, stats)
+    torch.cuda.synchronize()
+    assert torch.equal(o, o2)
