@@ -62,7 +62,9 @@
  *  W_qkv [d][3d] (output columns q | k | v, head h owning columns h*d/H ..
  *  (h+1)*d/H - 1 of each), W_o [d][d], ln2 gain [d], ln2 bias [d], W_1 [d][F],
  *  W_2 [F][d]; then the final LayerNorm gain [d] and bias [d] and the
- *  unembedding U [d][V].  No linear biases.  Each block is pre-LayerNorm:
+ *  unembedding U [d][V].  With n_kv_heads = K, W_qkv is [d][(H + 2K) d/H] (q heads | k
+ *  heads | v heads); with qk_norm the query heads' gain [d/H] and the key heads' gain
+ *  [d/H] follow W_qkv.  No linear biases.  Each block is pre-LayerNorm:
  *  h += Attn(LN1(h)) W_o, h += GELU(LN2(h) W_1) W_2, with causal softmax
  *  attention scaled by 1/sqrt(d/H) and rotary position embeddings on q and k
  *  (rotate-half pairing of head dims j and j + d/(2H), angle pos *
@@ -92,7 +94,12 @@
  *  Transformer: x (dev) int32 tokens [rows][seq + 1] row-major, ids in
  *  [0, vocab); sequence b predicts tokens[b][1..seq] from tokens[b][0..seq-1],
  *  so a batch has N = rows * seq loss rows (the mvp_out rows of
- *  mfmg_hvp_fwd_over_rev are ordered b * seq + s).  y is unused (may be NULL).
+ *  mfmg_hvp_fwd_over_rev are ordered b * seq + s).  y is unused (may be NULL),
+ *  unless docs (for the validation batch val_docs) = D > 0: then y (dev) int32 [D + 1]
+ *  are ascending offsets into the N loss rows, and tokens y[j] .. y[j + 1] - 1 are one
+ *  document, which attends to itself alone and whose rotary positions start at 0.
+ *  Offsets are clamped as in mfmg_seq_plan; tokens before y[0] and from y[D] on are
+ *  documents of their own.  Targets stay the next tokens of the rows.
  */
 #ifndef MFMG_H_
 #define MFMG_H_
@@ -193,6 +200,16 @@ typedef struct {
    * the last, or the last two.  The recomputation repeats the same kernels on the
    * same inputs, so results are bit-identical to 0. */
   int block_remat;
+  /* Transformer kind only: the attention of more recent decoders.  Any of the
+   * following other than 0 (and n_kv_heads other than n_heads) needs
+   * fused_attention = 1 and runs the attention operators below: both precisions,
+   * head dimensions that are multiples of 8 up to 128, any seq. */
+  int n_kv_heads;        /* key/value heads, a divisor of n_heads (0: n_heads) */
+  int qk_norm;           /* 1: RMS norms of query and key heads, epsilon ln_eps */
+  int rope_dims, rope_interleaved, rope_scaling;   /* as in mfmg_attn_desc, base rope_base */
+  float rope_factor, rope_train_len, rope_slow, rope_fast, rope_mscale;
+  int docs, val_docs;    /* documents of a training / validation batch (see "Batches"); 0:
+                            every row is one sequence */
 } mfmg_problem_desc;
 
 typedef struct mfmg_problem* mfmg_problem_t;

@@ -37,7 +37,10 @@ class mfmg_problem_desc(ctypes.Structure):
         ("d_model", c_int), ("n_heads", c_int), ("d_ff", c_int), ("vocab", c_int), ("seq", c_int),
         ("n_blocks", c_int), ("meta_hidden", c_int), ("ln_eps", c_float), ("rope_base", c_float),
         ("map_steps", c_int), ("ckpt_segment", c_int), ("fused_attention", c_int),
-        ("block_remat", c_int),
+        ("block_remat", c_int), ("n_kv_heads", c_int), ("qk_norm", c_int), ("rope_dims", c_int),
+        ("rope_interleaved", c_int), ("rope_scaling", c_int), ("rope_factor", c_float),
+        ("rope_train_len", c_float), ("rope_slow", c_float), ("rope_fast", c_float),
+        ("rope_mscale", c_float), ("docs", c_int), ("val_docs", c_int),
     ]
 
 

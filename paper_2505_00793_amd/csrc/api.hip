@@ -879,10 +879,12 @@ long n_eta_of(const mfmg_problem* p, int T) {
 bool aligned(const void* ptr, size_t a) { return (reinterpret_cast<uintptr_t>(ptr) % a) == 0; }
 
 mfmg_status check_batch(const mfmg_problem* p, const mfmg_batch* b, int rows, const char* what,
-                        int idx) {
+                        int idx, int docs) {
   if (!b) return fail(MFMG_ERR_INVALID_ARGUMENT, "%s[%d]: null batch", what, idx);
   if (!b->x || (!b->y && !p->tf))
     return fail(MFMG_ERR_INVALID_ARGUMENT, "%s[%d]: null x or y", what, idx);
+  if (p->tf && !b->y && docs)
+    return fail(MFMG_ERR_INVALID_ARGUMENT, "%s[%d]: null y (document offsets)", what, idx);
   if (b->rows != rows)
     return fail(MFMG_ERR_INVALID_ARGUMENT, "%s[%d]: rows %lld, expected %d", what, idx,
                 (long long)b->rows, rows);
@@ -1094,6 +1096,9 @@ mfmg_status mfmg_problem_create(const mfmg_problem_desc* desc, mfmg_problem_t* o
   if (d.fused_attention != 0 || d.block_remat != 0)
     return fail(MFMG_ERR_INVALID_ARGUMENT,
                 "fused_attention and block_remat apply to transformer problems");
+  if (d.n_kv_heads || d.qk_norm || d.rope_dims || d.rope_interleaved || d.rope_scaling || d.docs ||
+      d.val_docs)
+    return fail(MFMG_ERR_INVALID_ARGUMENT, "the attention options apply to transformer problems");
   if (d.optimizer != MFMG_OPT_SGD && d.optimizer != MFMG_OPT_ADAM)
     return fail(MFMG_ERR_INVALID_ARGUMENT, "unknown optimizer %d", d.optimizer);
   if (d.precision != MFMG_PREC_FP32 && d.precision != MFMG_PREC_BF16)
@@ -1202,7 +1207,7 @@ mfmg_status mfmg_inner_step(mfmg_problem_t p, const float* theta, const float* o
   if (batch->rows != p->d.rows)
     return fail(MFMG_ERR_INVALID_ARGUMENT, "batch rows %lld, expected %d", (long long)batch->rows,
                 p->d.rows);
-  TRY(check_batch(p, batch, p->d.rows, "batch", 0));
+  TRY(check_batch(p, batch, p->d.rows, "batch", 0, p->d.docs));
   TRY(check_align16({theta, opt_state, eta, theta_next, opt_state_next, grad_out}));
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (p->tf) {
@@ -1226,7 +1231,7 @@ mfmg_status mfmg_hvp_fwd_over_rev(mfmg_problem_t p, const float* theta, const fl
   if (!theta || !eta || !v || !hvp_out)
     return fail(MFMG_ERR_INVALID_ARGUMENT, "null theta, eta, v or hvp_out");
   if (step_index < 0) return fail(MFMG_ERR_INVALID_ARGUMENT, "negative step_index");
-  TRY(check_batch(p, batch, p->d.rows, "batch", 0));
+  TRY(check_batch(p, batch, p->d.rows, "batch", 0, p->d.docs));
   TRY(check_align16({theta, eta, v, grad_out, hvp_out}));
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (p->tf) {
@@ -1256,8 +1261,8 @@ mfmg_status check_meta_args(mfmg_problem_t p, const float* theta0, const float* 
   if ((!theta0 && p->d.meta != MFMG_META_MAML) || !eta || !d_eta_out)
     return fail(MFMG_ERR_INVALID_ARGUMENT, "null theta0, eta or d_eta_out");
   if (!train_batches) return fail(MFMG_ERR_INVALID_ARGUMENT, "null train_batches");
-  for (int t = 0; t < T; ++t) TRY(check_batch(p, &train_batches[t], p->d.rows, "train_batches", t));
-  TRY(check_batch(p, val_batch, p->d.val_rows, "val_batch", 0));
+  for (int t = 0; t < T; ++t) TRY(check_batch(p, &train_batches[t], p->d.rows, "train_batches", t, p->d.docs));
+  TRY(check_batch(p, val_batch, p->d.val_rows, "val_batch", 0, p->d.val_docs));
   TRY(check_align16({theta0, opt_state0, eta, d_eta_out}));
   size_t st = 0, dy = 0;
   *need = p->tf ? tf_meta_ws(p->d, T, &st, &dy) : meta_ws_bytes(p, T, &st, &dy);
@@ -1275,6 +1280,8 @@ mfmg_status meta_grad_run(mfmg_problem_t p, const float* theta0, const float* op
       const long n_eta = tf_n_eta(p->d);
       size_t b = need + 4 * (size_t)p->n_theta + 8 * (size_t)n_eta + (val_loss_out ? 4 : 0);
       b += (size_t)(T * p->d.rows + p->d.val_rows) * (p->d.seq + 1) * 4;
+      if (p->d.docs) b += 4 * (size_t)T * (p->d.docs + 1);
+      if (p->d.val_docs) b += 4 * ((size_t)p->d.val_docs + 1);
       *peak_bytes_out = b;
     }
     HIPCHK(tf_run_meta(p->d, theta0, eta, train_batches, T, val_batch, d_eta_out, val_loss_out,

@@ -23,6 +23,7 @@
 #include <type_traits>
 
 #include "kernels.h"
+#include "packed.h"
 #include "tf_engine.h"
 #include "transformer.h"
 
@@ -46,20 +47,58 @@ struct Carver {
 
 constexpr int MAXB = 16;
 
+// Whether a decoder's attention runs the packed operators (packed.hip, qkrope.hip):
+// grouped heads, norms, packed documents or other than plain rotations.
+bool packed_attention(const mfmg_problem_desc& D) {
+  return (D.n_kv_heads && D.n_kv_heads != D.n_heads) || D.qk_norm || D.rope_interleaved ||
+         (D.rope_dims && D.rope_dims != D.d_model / D.n_heads) || D.rope_scaling ||
+         (D.rope_mscale != 0.f && D.rope_mscale != 1.f) || D.docs || D.val_docs;
+}
+
+mfmg_attn_desc attn_desc_of(const mfmg_problem_desc& D) {
+  mfmg_attn_desc a;
+  std::memset(&a, 0, sizeof(a));
+  a.heads = D.n_heads;
+  a.kv_heads = D.n_kv_heads ? D.n_kv_heads : D.n_heads;
+  a.head_dim = D.d_model / D.n_heads;
+  a.precision = D.precision;
+  a.qk_norm = D.qk_norm;
+  a.norm_eps = D.ln_eps;
+  a.rope_dims = D.rope_dims;
+  a.rope_interleaved = D.rope_interleaved;
+  a.rope_base = D.rope_base;
+  a.rope_scaling = D.rope_scaling;
+  a.rope_factor = D.rope_factor;
+  a.rope_train_len = D.rope_train_len;
+  a.rope_slow = D.rope_slow;
+  a.rope_fast = D.rope_fast;
+  a.rope_mscale = D.rope_mscale;
+  return a;
+}
+
 struct Lay {
   int d, H, dh, F, V, S, Bt, Bv, L, mh, VE, fused, remat;
+  int K, QC;              // key heads; columns of a QKV row
+  int pk, norm;           // packed operators; query/key norms
+  int docs, vdocs;        // documents of a training / validation batch (0: its rows)
+  RopeFreqs freqs;        // (packed operators)
   // the weight gradients read their operands as stored by token (gemm_param_km),
   // so no transposed copies of them exist: bf16, every operand within gemm_km_fits
   bool km;
   float eps, lr;
   double base;
-  long emb, ln1g[MAXB], ln1b[MAXB], wqkv[MAXB], wo[MAXB], ln2g[MAXB], ln2b[MAXB], w1[MAXB],
+  long emb, ln1g[MAXB], ln1b[MAXB], wqkv[MAXB], qkg[MAXB], wo[MAXB], ln2g[MAXB], ln2b[MAXB], w1[MAXB],
       w2[MAXB], lnfg, lnfb, unemb, n;
   long ld(long x) const { return rup(x, VE); }
   int maxB() const { return std::max(Bt, Bv); }
-  // per-block matrices: 0 wqkv d->3d, 1 wo d->d, 2 w1 d->F, 3 w2 F->d
+  // sequences of a batch's plan
+  int seqs(bool val) const {
+    const int n = val ? vdocs : docs;
+    return n ? n + 2 : val ? Bv : Bt;
+  }
+  // per-block matrices: 0 wqkv d->QC, 1 wo d->d, 2 w1 d->F, 3 w2 F->d
   int in(int m) const { return m == 3 ? F : d; }
-  int out(int m) const { return m == 0 ? 3 * d : m == 2 ? F : d; }
+  int out(int m) const { return m == 0 ? QC : m == 2 ? F : d; }
   long woff(int b, int m) const { return m == 0 ? wqkv[b] : m == 1 ? wo[b] : m == 2 ? w1[b] : w2[b]; }
 };
 
@@ -76,9 +115,16 @@ Lay make_lay(const mfmg_problem_desc& D) {
   y.L = D.n_blocks;
   y.mh = D.meta_hidden;
   y.VE = D.precision == MFMG_PREC_BF16 ? 8 : 4;
+  y.K = D.n_kv_heads ? D.n_kv_heads : D.n_heads;
+  y.QC = (y.H + 2 * y.K) * y.dh;
+  y.pk = packed_attention(D);
+  y.norm = D.qk_norm;
+  y.docs = D.docs;
+  y.vdocs = D.val_docs;
+  if (y.pk) y.freqs = rope_freqs(attn_desc_of(D));
   y.fused = D.fused_attention;
   y.remat = D.block_remat;
-  y.km = y.VE == 8 && gemm_km_fits((long)y.maxB() * y.S, y.ld(std::max({3 * y.d, y.F, y.V})));
+  y.km = y.VE == 8 && gemm_km_fits((long)y.maxB() * y.S, y.ld(std::max({y.QC, y.F, y.V})));
   y.eps = D.ln_eps;
   y.lr = D.sgd_lr;
   y.base = D.rope_base;
@@ -89,7 +135,8 @@ Lay make_lay(const mfmg_problem_desc& D) {
   for (int b = 0; b < y.L; ++b) {
     y.ln1g[b] = o; o += d;
     y.ln1b[b] = o; o += d;
-    y.wqkv[b] = o; o += d * 3 * d;
+    y.wqkv[b] = o; o += d * y.QC;
+    y.qkg[b] = o; o += y.norm ? 2 * y.dh : 0;
     y.wo[b] = o; o += d * d;
     y.ln2g[b] = o; o += d;
     y.ln2b[b] = o; o += d;
@@ -108,6 +155,7 @@ struct Ops {  // operand copies of a parameter vector (theta_t or a tangent)
   T* W[MAXB][4];
   T* WT[MAXB][4];
   float* ln[MAXB][4];  // ln1 g, ln1 b, ln2 g, ln2 b
+  float* qk[MAXB];     // [2][dh] query and key gains (with norms)
   float* lnf[2];
   T* U;
   T* UT;
@@ -122,6 +170,7 @@ void carve_ops(const Lay& y, Carver& c, Ops<T>& o) {
       o.WT[b][m] = c.take<T>((size_t)y.out(m) * y.ld(y.in(m)));
     }
     for (int k = 0; k < 4; ++k) o.ln[b][k] = c.take<float>(y.d);
+    o.qk[b] = y.norm ? c.take<float>(2 * y.dh) : nullptr;
   }
   o.lnf[0] = c.take<float>(y.d);
   o.lnf[1] = c.take<float>(y.d);
@@ -156,6 +205,13 @@ struct Act {  // one inner step at up to maxB sequences (the dynamic memory)
   float *P32[MAXB], *Pd32[MAXB];                 // materialised attention only
   T *Pb[MAXB], *PbT[MAXB], *Pdb[MAXB], *PdbT[MAXB];
   float *lse[MAXB], *cst[MAXB], *ar, *ard;       // fused attention only: per query row
+  // packed operators: QKV rows before (float32; every block's own with norms, whose
+  // backward reads them) and after the rotation, their gradient, the gains' partial
+  // sums, the plan of the batch's sequences
+  float *X[MAXB], *Xd[MAXB];
+  T *Y[MAXB], *Yd[MAXB], *dY, *dYd;
+  float* qkpart;
+  char* plan;
   T *O[MAXB], *OT[MAXB], *Od[MAXB], *OdT[MAXB];
   float *Z1[MAXB], *Z1d[MAXB];
   T *A1[MAXB], *A1T[MAXB], *A1d[MAXB], *A1dT[MAXB];
@@ -193,7 +249,7 @@ void carve_act_bufs(const Lay& y, Carver& c, Act<T>& a, int sets, bool all) {
   // transposed weight-gradient operands
   auto OPTW = [&](long n) -> T* { return all || !y.km ? c.take<T>(n) : nullptr; };
   // transposed and float32 per-head operands: materialised attention only
-  const bool mat = all || !y.fused;
+  const bool mat = (all || !y.fused) && !y.pk;
   auto OPTM = [&](long n) -> T* { return mat ? c.take<T>(n) : nullptr; };
   auto F32M = [&](long n) -> float* { return mat ? c.take<float>(n) : nullptr; };
   a.ids = c.take<int>(N);
@@ -226,6 +282,7 @@ void carve_act_bufs(const Lay& y, Carver& c, Act<T>& a, int sets, bool all) {
       a.P32[b] = a.P32[b - sets]; a.Pd32[b] = a.Pd32[b - sets];
       a.Pb[b] = a.Pb[b - sets]; a.PbT[b] = a.PbT[b - sets]; a.Pdb[b] = a.Pdb[b - sets]; a.PdbT[b] = a.PdbT[b - sets];
       a.lse[b] = a.lse[b - sets]; a.cst[b] = a.cst[b - sets];
+      a.X[b] = a.X[b - sets]; a.Xd[b] = a.Xd[b - sets]; a.Y[b] = a.Y[b - sets]; a.Yd[b] = a.Yd[b - sets];
       a.O[b] = a.O[b - sets]; a.OT[b] = a.OT[b - sets]; a.Od[b] = a.Od[b - sets]; a.OdT[b] = a.OdT[b - sets];
       a.Z1[b] = a.Z1[b - sets]; a.Z1d[b] = a.Z1d[b - sets];
       a.A1[b] = a.A1[b - sets]; a.A1T[b] = a.A1T[b - sets]; a.A1d[b] = a.A1d[b - sets]; a.A1dT[b] = a.A1dT[b - sets];
@@ -237,12 +294,21 @@ void carve_act_bufs(const Lay& y, Carver& c, Act<T>& a, int sets, bool all) {
     a.a1d[b] = OPT(N * y.ld(d)); a.a1dT[b] = OPTW(d * y.ld(N));
     a.a2[b] = OPT(N * y.ld(d)); a.a2T[b] = OPTW(d * y.ld(N));
     a.a2d[b] = OPT(N * y.ld(d)); a.a2dT[b] = OPTW(d * y.ld(N));
-    a.Q[b] = OPT(BH * hrow); a.QT[b] = OPTM(BH * hcol);
-    a.K[b] = OPT(BH * hrow); a.KT[b] = OPTM(BH * hcol);
-    a.Vv[b] = OPT(BH * hrow); a.VT[b] = OPTM(BH * hcol);
-    a.Qd[b] = OPT(BH * hrow); a.QdT[b] = OPTM(BH * hcol);
-    a.Kd[b] = OPT(BH * hrow); a.KdT[b] = OPTM(BH * hcol);
-    a.Vd[b] = OPT(BH * hrow); a.VdT[b] = OPTM(BH * hcol);
+    auto OPTH = [&](long n) -> T* { return y.pk ? nullptr : c.take<T>(n); };
+    a.Q[b] = OPTH(BH * hrow); a.QT[b] = OPTM(BH * hcol);
+    a.K[b] = OPTH(BH * hrow); a.KT[b] = OPTM(BH * hcol);
+    a.Vv[b] = OPTH(BH * hrow); a.VT[b] = OPTM(BH * hcol);
+    a.Qd[b] = OPTH(BH * hrow); a.QdT[b] = OPTM(BH * hcol);
+    a.Kd[b] = OPTH(BH * hrow); a.KdT[b] = OPTM(BH * hcol);
+    a.Vd[b] = OPTH(BH * hrow); a.VdT[b] = OPTM(BH * hcol);
+    a.X[b] = a.Xd[b] = nullptr;
+    a.Y[b] = a.Yd[b] = nullptr;
+    if (y.pk) {
+      if (y.norm) {
+        a.X[b] = F32(N * y.QC); a.Xd[b] = F32(N * y.QC);
+      }
+      a.Y[b] = OPT(N * y.ld(y.QC)); a.Yd[b] = OPT(N * y.ld(y.QC));
+    }
     if (y.fused) {
       a.P32[b] = a.Pd32[b] = nullptr;
       a.Pb[b] = a.PbT[b] = a.Pdb[b] = a.PdbT[b] = nullptr;
@@ -264,7 +330,27 @@ void carve_act_bufs(const Lay& y, Carver& c, Act<T>& a, int sets, bool all) {
   a.afd = OPT(N * y.ld(d)); a.afdT = OPTW(d * y.ld(N));
   a.logits = F32(N * y.V); a.logitsd = F32(N * y.V);
   a.y32 = F32(N * std::max(d, F)); a.yd32 = F32(N * std::max(d, F));
-  a.qkv32 = F32(N * 3 * d); a.qkvd32 = F32(N * 3 * d);
+  a.qkv32 = F32(N * y.QC); a.qkvd32 = F32(N * y.QC);
+  a.dY = a.dYd = nullptr;
+  a.qkpart = nullptr;
+  a.plan = nullptr;
+  if (y.pk) {
+    for (int b = 0; b < y.L && !y.norm; ++b) {
+      a.X[b] = a.qkv32;
+      a.Xd[b] = a.qkvd32;
+    }
+    a.dY = OPT(N * y.ld(y.QC)); a.dYd = OPT(N * y.ld(y.QC));
+    if (y.norm) {
+      // (parts do not grow steadily with the rows)
+      const int parts = std::max(qk_rope_parts((long)y.Bt * S, y.H, y.K, y.dh),
+                                 qk_rope_parts((long)y.Bv * S, y.H, y.K, y.dh));
+      a.qkpart = F32((long)parts * 4 * y.dh);
+    }
+    size_t pt = 0, pv = 0;
+    seq_plan_at(nullptr, (long)y.Bt * S, y.seqs(false), &pt);
+    seq_plan_at(nullptr, (long)y.Bv * S, y.seqs(true), &pv);
+    a.plan = c.take<char>(std::max(pt, pv));
+  }
   a.Qh = F32M(N * d); a.Kh = F32M(N * d); a.Vh = F32M(N * d);
   a.Qdh = F32M(N * d); a.Kdh = F32M(N * d); a.Vdh = F32M(N * d);
   if (y.fused) {
@@ -283,7 +369,7 @@ void carve_act_bufs(const Lay& y, Carver& c, Act<T>& a, int sets, bool all) {
   a.dh = F32(N * d); a.dhd = F32(N * d);
   a.dhb = OPT(N * y.ld(d)); a.dhbT = OPTW(d * y.ld(N));
   a.dhdb = OPT(N * y.ld(d)); a.dhdbT = OPTW(d * y.ld(N));
-  const long FQ = std::max(F, 3 * d);  // also holds the dqkv operands
+  const long FQ = std::max(F, (long)y.QC);  // also holds the dqkv operands
   a.dZ1 = OPT(N * y.ld(FQ)); a.dZ1T = OPTW(FQ * y.ld(N));
   a.dZ1d = OPT(N * y.ld(FQ)); a.dZ1dT = OPTW(FQ * y.ld(N));
   a.dOh = OPT(BH * hrow); a.dOhT = OPTM(BH * hcol);
@@ -293,7 +379,7 @@ void carve_act_bufs(const Lay& y, Carver& c, Act<T>& a, int sets, bool all) {
   a.ts = carve_segs(c, N, y.V);
   a.epart = F32(nsm * 2 * d);
   a.skws_n = std::max({gemm_splitk_floats(F, d, (int)N), gemm_splitk_floats(d, F, (int)N),
-                       gemm_splitk_floats(d, d, (int)N), gemm_splitk_floats(d, 3 * d, (int)N),
+                       gemm_splitk_floats(d, d, (int)N), gemm_splitk_floats(d, y.QC, (int)N),
                        gemm_splitk_floats(d, y.V, (int)N)});
   a.skws = F32(a.skws_n);
   a.loss_rows = F32(N);
@@ -460,6 +546,68 @@ struct TfEng {
     t.scale = 1.0f / std::sqrt((float)y.dh);
     return t;
   }
+  // The packed operators' arguments for block b of a batch of Bn rows (val: its plan).
+  SeqPlan plan_of(int Bn, bool val, const Act<T>& a) const {
+    return seq_plan_at(a.plan, (long)Bn * y.S, y.seqs(val), nullptr);
+  }
+  // The plan of a batch: its documents, which may be any split of its loss rows, or
+  // its rows.
+  hipError_t make_plan(const mfmg_batch* batch, int Bn, bool val, const Act<T>& a) const {
+    if (!y.pk) return hipSuccess;
+    const bool docs = val ? y.vdocs : y.docs;
+    SeqPlanArgs p;
+    p.cu = docs ? static_cast<const int*>(batch->y) : nullptr;
+    p.positions = nullptr;
+    p.cover = docs;
+    p.len = y.S;
+    p.p = plan_of(Bn, val, a);
+    return seq_plan_make(p, s);
+  }
+  QkRopeArgs<T> rope_args(const Ops<T>& th, const Ops<T>* v, int b, int Bn, bool val,
+                          const Act<T>& a) const {
+    QkRopeArgs<T> r;
+    std::memset(&r, 0, sizeof(r));
+    r.x = a.X[b]; r.xd = a.Xd[b]; r.ldx = r.ldxd = y.QC;
+    r.gain = th.qk[b]; r.gaind = v ? v->qk[b] : nullptr;
+    r.ldy = r.ldyd = r.lddx = r.lddxd = y.ld(y.QC);
+    r.p = plan_of(Bn, val, a);
+    r.H = y.H; r.K = y.K; r.dh = y.dh; r.dual = v != nullptr;
+    r.eps = y.eps;
+    r.partial = a.qkpart;
+    r.f = y.freqs;
+    return r;
+  }
+  PackedAttnArgs<T> packed_args(int b, int Bn, bool val, bool dual, const Act<T>& a) const {
+    PackedAttnArgs<T> t;
+    std::memset(&t, 0, sizeof(t));
+    const long ld = y.ld(y.QC), k = (long)y.H * y.dh, v = k + (long)y.K * y.dh;
+    t.q = a.Y[b]; t.k = a.Y[b] + k; t.v = a.Y[b] + v;
+    t.dq = a.dY; t.dk = a.dY + k; t.dv = a.dY + v;
+    t.o = a.O[b]; t.g = a.dOh;
+    if (dual) {
+      t.qd = a.Yd[b]; t.kd = a.Yd[b] + k; t.vd = a.Yd[b] + v;
+      t.dqd = a.dYd; t.dkd = a.dYd + k; t.dvd = a.dYd + v;
+      t.od = a.Od[b]; t.gd = a.dOdh;
+    }
+    t.ldq = t.ldk = t.ldv = t.ldqd = t.ldkd = t.ldvd = ld;
+    t.lddq = t.lddk = t.lddv = t.lddqd = t.lddkd = t.lddvd = ld;
+    t.ldo = t.ldod = t.ldg = t.ldgd = y.ld(y.d);
+    t.lse = a.lse[b]; t.cst = a.cst[b]; t.r = a.ar; t.rd = a.ard;
+    t.p = plan_of(Bn, val, a);
+    t.H = y.H; t.K = y.K; t.dh = y.dh; t.dual = dual;
+    t.scale = 1.0f / std::sqrt((float)y.dh);
+    return t;
+  }
+  // Transposed copies (where the plan has them) of operand rows the packed operators
+  // wrote: by wgrad_copy, or for float32 operands from the rows themselves.
+  hipError_t packed_copy(const T* x, const T* xd, int N, int cols, T* xT, T* xdT) const {
+    if constexpr (std::is_same<T, float>::value) {
+      HC(convert_matrix<float>(x, N, cols, (int)y.ld(cols), nullptr, 0, xT, (int)y.ld(N), s));
+      if (xd) HC(convert_matrix<float>(xd, N, cols, (int)y.ld(cols), nullptr, 0, xdT, (int)y.ld(N), s));
+      return hipSuccess;
+    }
+    return wgrad_copy(x, xd, N, cols, xT, xdT);
+  }
   static int fl(bool dual, bool ad = true) {
     return G_C1 | (dual ? (G_BD | (ad ? G_AD : 0)) : 0);
   }
@@ -526,6 +674,7 @@ struct TfEng {
                              (int)y.ld(y.out(m)), o.WT[b][m], (int)y.ld(y.in(m)), s));
       const long offs[4] = {y.ln1g[b], y.ln1b[b], y.ln2g[b], y.ln2b[b]};
       for (int k = 0; k < 4; ++k) HC(copy(th + offs[k], o.ln[b][k], y.d, s));
+      if (y.norm) HC(copy(th + y.qkg[b], o.qk[b], 2 * y.dh, s));
     }
     HC(copy(th + y.lnfg, o.lnf[0], y.d, s));
     HC(copy(th + y.lnfb, o.lnf[1], y.d, s));
@@ -584,11 +733,12 @@ struct TfEng {
 
   // ------------------------------------------------------------ forward
   // Forward (dual when v) of Bn sequences through the decoder up to the logits.
-  hipError_t forward(const Ops<T>& th, const Ops<T>* v, int Bn, const Act<T>& a) const {
+  // val: the batch is the validation batch (the plan in use is its).
+  hipError_t forward(const Ops<T>& th, const Ops<T>* v, int Bn, bool val, const Act<T>& a) const {
     const bool dual = v != nullptr;
     const int d = y.d, N = Bn * y.S;
     HC(gather_rows(a.ids, N, d, th.emb, dual ? v->emb : nullptr, a.h[0], dual ? a.hd[0] : nullptr, s));
-    for (int b = 0; b < y.L; ++b) HC(block_forward(th, v, Bn, b, true, a));
+    for (int b = 0; b < y.L; ++b) HC(block_forward(th, v, Bn, val, b, true, a));
     // final LayerNorm -> af, logits = af U
     LnArgs ln;
     ln.x = a.h[2 * y.L]; ln.xd = a.hd[2 * y.L];
@@ -606,7 +756,7 @@ struct TfEng {
   // Block b's forward from its input h[2b] (and tangent): everything its
   // backward reads, and with `output` also the block's output h[2b + 2] (the
   // rematerialising pass before the block's backward skips that last product).
-  hipError_t block_forward(const Ops<T>& th, const Ops<T>* v, int Bn, int b, bool output,
+  hipError_t block_forward(const Ops<T>& th, const Ops<T>* v, int Bn, bool val, int b, bool output,
                            const Act<T>& a) const {
     const bool dual = v != nullptr;
     const int d = y.d, S = y.S, H = y.H, dh = y.dh, F = y.F;
@@ -623,7 +773,14 @@ struct TfEng {
       ln.rstd = a.rs1[b]; ln.c = a.c1[b]; ln.N = N; ln.d = d; ln.dual = dual; ln.eps = y.eps;
       HC(ln_operands(ln, a.a1[b], a.a1d[b], a.a1T[b], a.a1dT[b]));
       // qkv = a1 Wqkv, rotated by RoPE, per head
-      if (y.fused) {
+      if (y.pk) {
+        HC(store(op(a.a1[b], dual ? a.a1d[b] : nullptr, th.WT[b][0], dual ? v->WT[b][0] : nullptr,
+                    (int)y.ld(d), (int)y.ld(d), N, y.QC, d),
+                 fl(dual), a.X[b], a.Xd[b], y.QC, 0, 1.0f, dual));
+        QkRopeArgs<T> r = rope_args(th, v, b, Bn, val, a);
+        r.y = a.Y[b]; r.yd = a.Yd[b];
+        HC(qk_rope_fwd(r, s));
+      } else if (y.fused) {
         if constexpr (std::is_same<T, bf16_t>::value) {
           // straight from the product's epilogue (4096 tokens, d 512, dual: 39.7 us; the
           // float32 product and a split kernel took 38.8 + 12.4 us)
@@ -674,7 +831,10 @@ struct TfEng {
                    S, dh, BH, sh, hrow, hcol));
         }
       }
-      if (y.fused) {
+      if (y.pk) {
+        HC(packed_attn_fwd(packed_args(b, Bn, val, dual, a), s));
+        HC(packed_copy(a.O[b], dual ? a.Od[b] : nullptr, N, d, a.OT[b], a.OdT[b]));
+      } else if (y.fused) {
         HC(attn_fwd(attn_args(b, Bn, dual, a), s));
         HC(wgrad_copy(a.O[b], dual ? a.Od[b] : nullptr, N, d, a.OT[b], a.OdT[b]));
       } else {
@@ -760,7 +920,7 @@ struct TfEng {
   // out: operand copies to write from the parameter epilogue (or null).
   // segs: where the batch's sorted tokens go (null: the step workspace's);
   // sorted: they are already there (the same batch was sorted by an earlier pass).
-  hipError_t backward(const Ops<T>& th, const Ops<T>* v, int Bn, ParamArgs<T> P,
+  hipError_t backward(const Ops<T>& th, const Ops<T>* v, int Bn, bool val, ParamArgs<T> P,
                       const Ops<T>* out, const Act<T>& a, const TokenSegs* segs = nullptr,
                       bool sorted = false) const {
     const bool dual = v != nullptr;
@@ -805,7 +965,7 @@ struct TfEng {
       // block rematerialisation: the shared sets hold the last blocks' activations
       // from the forward; every other block is recomputed from its input h[2b]
       // before its backward
-      if (y.remat && b < y.L - a.sets) HC(block_forward(th, v, Bn, b, false, a));
+      if (y.remat && b < y.L - a.sets) HC(block_forward(th, v, Bn, val, b, false, a));
       // ---- MLP: h_out = h_mid + GELU(a2 W1) W2
       HC(dh_operands(N, dual, a));
       HC(wgrad(a.A1[b], a.A1d[b], a.A1T[b], a.A1dT[b], a.dhb, a.dhdb, a.dhbT, a.dhdbT, F, d, N, dual,
@@ -837,11 +997,25 @@ struct TfEng {
         e.Oh = a.dOh; e.OhT = a.dOhT; e.Odh = a.dOdh; e.OdhT = a.dOdhT;
         e.ldh = (int)y.ld(dh); e.ldhT = (int)y.ld(S);
         e.seq = S; e.heads = H; e.dh = dh; e.M = N; e.N = d; e.dual = dual;
+        if (y.pk) {   // rows by token: one head of the model's width
+          e.ldh = (int)y.ld(d);
+          e.seq = N; e.heads = 1; e.dh = d;
+        }
         HC(gemm_head_split<T>(op(a.dhb, dual ? a.dhdb : nullptr, th.W[b][1], dual ? v->W[b][1] : nullptr,
                                  (int)y.ld(d), (int)y.ld(d), N, d, d),
                               fl(dual), e, s));
       }
-      if (y.fused) {
+      if (y.pk) {
+        HC(packed_attn_bwd(packed_args(b, Bn, val, dual, a), s));
+        QkRopeArgs<T> r = rope_args(th, v, b, Bn, val, a);
+        r.y = a.dY; r.yd = a.dYd;
+        r.dx = a.dZ1; r.dxd = a.dZ1d;
+        HC(qk_rope_bwd(r, s));
+        if (y.norm)
+          HC(gain_param<T>(a.qkpart, qk_rope_parts(N, H, y.K, dh), dh, y.qkg[b], y.qkg[b] + dh, P,
+                           out ? out->qk[b] : nullptr, out ? out->qk[b] + dh : nullptr, s));
+        HC(packed_copy(a.dZ1, dual ? a.dZ1d : nullptr, N, y.QC, a.dZ1T, a.dZ1dT));
+      } else if (y.fused) {
         HC(attn_bwd(attn_args(b, Bn, dual, a), s));
         HC(wgrad_copy(a.dZ1, dual ? a.dZ1d : nullptr, N, 3 * d, a.dZ1T, a.dZ1dT));
       } else {
@@ -899,11 +1073,11 @@ struct TfEng {
                    3 * d));
         }
       }
-      HC(wgrad(a.a1[b], a.a1d[b], a.a1T[b], a.a1dT[b], a.dZ1, a.dZ1d, a.dZ1T, a.dZ1dT, d, 3 * d, N,
+      HC(wgrad(a.a1[b], a.a1d[b], a.a1T[b], a.a1dT[b], a.dZ1, a.dZ1d, a.dZ1T, a.dZ1dT, d, y.QC, N,
                dual,
-               matP(y.wqkv[b], d, 3 * d, out ? out->W[b][0] : nullptr, out ? out->WT[b][0] : nullptr), a));
+               matP(y.wqkv[b], d, y.QC, out ? out->W[b][0] : nullptr, out ? out->WT[b][0] : nullptr), a));
       HC(store(op(a.dZ1, dual ? a.dZ1d : nullptr, th.W[b][0], dual ? v->W[b][0] : nullptr,
-                  (int)y.ld(3 * d), (int)y.ld(3 * d), N, d, 3 * d),
+                  (int)y.ld(y.QC), (int)y.ld(y.QC), N, d, y.QC),
                fl(dual), a.y32, a.yd32, d, 0, 1.0f, dual));
       HC(ln_bwd_call(a.y32, a.yd32, a.xh1[b], a.xhd1[b], a.rs1[b], a.c1[b], th.ln[b][0],
                      dual ? v->ln[b][0] : nullptr, a.dh, dual ? a.dhd : nullptr, y.ln1g[b], y.ln1b[b],
@@ -940,7 +1114,7 @@ hipError_t run_meta_t(const Lay& y, const float* theta0, const float* eta,
   TfEng<T> E{y, eta, s};
   const Act<T>& a = p.act;
   const int Nt = y.Bt * y.S;
-  HC(rope_table(y.S, y.dh, y.base, a.cs, a.sn, s));
+  if (!y.pk) HC(rope_table(y.S, y.dh, y.base, a.cs, a.sn, s));
   HC(E.to_ops(theta0, p.slot[0]));
   // meta-model inputs: rows of the initial embedding table at every step's tokens
   for (int t = 0; t < T_; ++t) {
@@ -951,33 +1125,36 @@ hipError_t run_meta_t(const Lay& y, const float* theta0, const float* eta,
   // forward unroll
   for (int t = 0; t < T_; ++t) {
     HC(split_tokens(static_cast<const int*>(batches[t].x), y.Bt, y.S, y.V, a.ids, a.labels, s));
-    HC(E.forward(p.slot[t], nullptr, y.Bt, a));
+    HC(E.make_plan(&batches[t], y.Bt, false, a));
+    HC(E.forward(p.slot[t], nullptr, y.Bt, false, a));
     HC(E.head(y.Bt, false, p.meta.u + (long)t * Nt, nullptr, nullptr, a));
     ParamArgs<T> P = pbase<T>(y, P_UPD_SGD_FIXED, eta);
     P.theta = t == 0 ? theta0 : p.run[(t - 1) & 1];
     P.theta_next = p.run[t & 1];
-    HC(E.backward(p.slot[t], nullptr, y.Bt, P, &p.slot[t + 1], a, &p.segs[t], false));
+    HC(E.backward(p.slot[t], nullptr, y.Bt, false, P, &p.slot[t + 1], a, &p.segs[t], false));
   }
   // outer loss and seed
   {
     const int Nv = y.Bv * y.S;
     HC(split_tokens(static_cast<const int*>(val->x), y.Bv, y.S, y.V, a.ids, a.labels, s));
-    HC(E.forward(p.slot[T_], nullptr, y.Bv, a));
+    HC(E.make_plan(val, y.Bv, true, a));
+    HC(E.forward(p.slot[T_], nullptr, y.Bv, true, a));
     HC(E.head(y.Bv, false, nullptr, nullptr, nullptr, a));
     if (val_loss) HC(loss_reduce(a.loss_rows, nullptr, Nv, 1.0f / Nv, val_loss, s));
     ParamArgs<T> P = pbase<T>(y, P_SEED_SGD_FIXED, eta);
     P.thetabar = p.thetabar;
-    HC(E.backward(p.slot[T_], nullptr, y.Bv, P, &p.v[0], a));
+    HC(E.backward(p.slot[T_], nullptr, y.Bv, true, P, &p.v[0], a));
   }
   // reverse sweep
   int vc = 0;
   for (int i = T_ - 1; i >= 0; --i) {
     HC(split_tokens(static_cast<const int*>(batches[i].x), y.Bt, y.S, y.V, a.ids, a.labels, s));
-    HC(E.forward(p.slot[i], &p.v[vc], y.Bt, a));
+    HC(E.make_plan(&batches[i], y.Bt, false, a));
+    HC(E.forward(p.slot[i], &p.v[vc], y.Bt, false, a));
     HC(E.head(y.Bt, true, p.meta.u + (long)i * Nt, nullptr, p.meta.ubar + (long)i * Nt, a));
     ParamArgs<T> P = pbase<T>(y, P_REV_SGD_FIXED, eta);
     P.thetabar = p.thetabar;
-    HC(E.backward(p.slot[i], &p.v[vc], y.Bt, P, i > 0 ? &p.v[vc ^ 1] : nullptr, a, &p.segs[i],
+    HC(E.backward(p.slot[i], &p.v[vc], y.Bt, false, P, i > 0 ? &p.v[vc ^ 1] : nullptr, a, &p.segs[i],
                   true));
     vc ^= 1;
   }
@@ -1001,18 +1178,19 @@ hipError_t run_inner_t(const Lay& y, const float* theta, const float* eta, const
   TfEng<T> E{y, eta, s};
   const Act<T>& a = p.act;
   const int N = y.Bt * y.S;
-  HC(rope_table(y.S, y.dh, y.base, a.cs, a.sn, s));
+  if (!y.pk) HC(rope_table(y.S, y.dh, y.base, a.cs, a.sn, s));
   HC(E.to_ops(theta, p.th));
   HC(split_tokens(static_cast<const int*>(b->x), y.Bt, y.S, y.V, a.ids, a.labels, s));
   HC(meta_alpha_step(y, E, theta, p.meta, a));
-  HC(E.forward(p.th, nullptr, y.Bt, a));
+  HC(E.make_plan(b, y.Bt, false, a));
+  HC(E.forward(p.th, nullptr, y.Bt, false, a));
   HC(E.head(y.Bt, false, p.meta.u, nullptr, nullptr, a));
   if (loss_out) HC(loss_reduce(a.loss_rows, p.meta.u, N, 1.0f / N, loss_out, s));
   ParamArgs<T> P = pbase<T>(y, P_UPD_SGD_FIXED, eta);
   P.theta = theta;
   P.theta_next = theta_next;
   P.grad_out = grad_out;
-  return E.backward(p.th, nullptr, y.Bt, P, nullptr, a);
+  return E.backward(p.th, nullptr, y.Bt, false, P, nullptr, a);
 }
 
 template <typename T>
@@ -1023,17 +1201,18 @@ hipError_t run_hvp_t(const Lay& y, const float* theta, const float* eta, const m
   plan_step_t(y, ws, p);
   TfEng<T> E{y, eta, s};
   const Act<T>& a = p.act;
-  HC(rope_table(y.S, y.dh, y.base, a.cs, a.sn, s));
+  if (!y.pk) HC(rope_table(y.S, y.dh, y.base, a.cs, a.sn, s));
   HC(E.to_ops(theta, p.th));
   HC(E.to_ops(v, p.v));
   HC(split_tokens(static_cast<const int*>(b->x), y.Bt, y.S, y.V, a.ids, a.labels, s));
   HC(meta_alpha_step(y, E, theta, p.meta, a));
-  HC(E.forward(p.th, &p.v, y.Bt, a));
+  HC(E.make_plan(b, y.Bt, false, a));
+  HC(E.forward(p.th, &p.v, y.Bt, false, a));
   HC(E.head(y.Bt, true, p.meta.u, mvp_out, nullptr, a));
   ParamArgs<T> P = pbase<T>(y, P_HVP, eta);
   P.grad_out = grad_out;
   P.hvp_out = hvp_out;
-  return E.backward(p.th, &p.v, y.Bt, P, nullptr, a);
+  return E.backward(p.th, &p.v, y.Bt, false, P, nullptr, a);
 }
 
 }  // namespace
@@ -1060,6 +1239,17 @@ const char* tf_validate(const mfmg_problem_desc& D) {
     return "ln_eps and rope_base must be > 0, sgd_lr finite";
   if (D.fused_attention != 0 && D.fused_attention != 1) return "fused_attention must be 0 or 1";
   if (D.block_remat != 0 && D.block_remat != 1) return "block_remat must be 0 or 1";
+  if (D.docs < 0 || D.docs > D.rows * D.seq || D.val_docs < 0 || D.val_docs > D.val_rows * D.seq)
+    return "docs (val_docs) must be in [0, tokens of the batch]";
+  if (packed_attention(D)) {
+    if (!D.fused_attention)
+      return "grouped heads, query/key norms, documents and rotary options need fused_attention";
+    if (const char* msg = attn_desc_error(attn_desc_of(D))) return msg;
+    const Lay y = make_lay(D);
+    if (y.VE == 8 && !y.km && ((long)D.rows * D.seq % 8 || (long)D.val_rows * D.seq % 8))
+      return "a vocabulary this large needs a multiple of 8 tokens a batch";
+    return nullptr;
+  }
   if (D.fused_attention &&
       (D.precision != MFMG_PREC_BF16 || !attn_fused_supported(D.seq, dh)))
     return "fused attention needs bf16 operands, head dim 64 and seq a multiple of 64";
