@@ -965,7 +965,7 @@ mfmg_status check_gains(const mfmg_attn* a, const float* gain, const float* gain
 }
 
 size_t attn_ws_bytes(const mfmg_attn* a, int64_t n) {
-  size_t w = 8 * (size_t)a->d.heads * (size_t)n;   // r and rd of the attention backward
+  size_t w = 4 * packed_attn_ws_floats(n, a->d.heads, a->d.kv_heads, a->d.head_dim);
   if (a->d.qk_norm && n > 0)
     w = std::max(w, 16 * (size_t)a->d.head_dim *
                         (size_t)qk_rope_parts(n, a->d.heads, a->d.kv_heads, a->d.head_dim));
@@ -1526,8 +1526,7 @@ mfmg_status run_attn_bwd(PackedAttnArgs<T> p, const void* o, const void* od, int
     p.dqd = (T*)dxd->q; p.dkd = (T*)dxd->k; p.dvd = (T*)dxd->v;
     p.lddqd = dxd->ldq; p.lddkd = dxd->ldk; p.lddvd = dxd->ldv;
   }
-  p.r = static_cast<float*>(ws);
-  p.rd = p.r + (long)p.H * p.p.n;
+  packed_attn_ws(p, static_cast<float*>(ws));
   HIPCHK(packed_attn_bwd(p, s));
   return MFMG_OK;
 }

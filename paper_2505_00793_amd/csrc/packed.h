@@ -6,7 +6,9 @@
 
 namespace mfmg {
 
-constexpr int PK_TILE = 128;        // rows (queries or keys) of an attention tile
+// Attention tiles of two sizes: 64 and 128 rows (queries or keys).
+__host__ __device__ constexpr int tile_rows(int kind) { return kind ? 128 : 64; }
+__host__ __device__ constexpr int tile_kind(int rows) { return rows == 128 ? 1 : 0; }
 constexpr int PK_MAX_DH = 128;      // largest head dimension
 constexpr long PK_MAX_TOKENS = (1L << 31) - 1024;
 constexpr int PK_MAX_SEQS = 1 << 24;
@@ -15,14 +17,19 @@ constexpr int ROPE_MAX_PAIRS = PK_MAX_DH / 2;
 
 // What the kernels need to know of a batch's sequences, in device memory.
 // Sequences are [b[j], b[j + 1]), j < m; tokens outside [b[0], b[m]) are unused rows.
-struct SeqPlan {
-  int* head;      // [4] tiles, b[0], b[m], 0
-  int* bound;     // [m + 1] b
+// A tile is (first row, b[j], b[j + 1], 0) of its sequence j; the lists are longest first.
+struct TileList {
   int* tstart;    // [m + 1] tiles before sequence j
-  int4* tile;     // [max_tiles] first row, b[j], b[j + 1], 0 of each tile
+  int4* byq;      // [max_tiles] as query tiles, by the keys they see
+  int4* byk;      // [max_tiles] as key tiles, by the queries that see them
+};
+struct SeqPlan {
+  int* head;      // [4] tiles of 64 rows, of 128 rows, b[0], b[m]
+  int* bound;     // [m + 1] b
   int* pos;       // [n] rotary position of each token
+  TileList list[2];
   long n;
-  int m, max_tiles;
+  int m, max_tiles[2];
 };
 // Layout of a plan over n tokens and m sequences at `base` (null: measure);
 // *bytes receives its size.
@@ -55,10 +62,17 @@ struct PackedAttnArgs {
   float* lse;                     // [H][n] log2 of the softmax denominators, scaled scores' base 2
   float* cst;                     // [H][n] <P, Sd> (dual)
   float *r, *rd;                  // [H][n] backward workspace: <dO, O>, <dOd, O> + <dO, Od>
+  float* partial;                 // [parts][n][K][2 or 4][dh] backward workspace: dK, dV (and
+  int parts;                      //   tangents) of parts of the query heads (parts > 1)
   SeqPlan p;
   int H, K, dh, dual;
   float scale;
 };
+// Floats of the backward's workspace, and its parts (r, rd, partial, parts of a, whose n, H,
+// K are set) at `ws`.
+size_t packed_attn_ws_floats(long n, int H, int K, int dh);
+template <typename T>
+void packed_attn_ws(PackedAttnArgs<T>& a, float* ws);
 template <typename T>
 hipError_t packed_attn_fwd(const PackedAttnArgs<T>& a, hipStream_t s);
 template <typename T>

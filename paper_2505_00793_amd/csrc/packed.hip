@@ -36,7 +36,7 @@ namespace mfmg {
 
 namespace {
 
-constexpr int KB = 64;   // rows of a block staged in LDS
+constexpr int SB = 32;   // rows of a staged block that a wave forms and consumes scores of at a time
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 template <int R> struct AccT;
@@ -68,13 +68,12 @@ __device__ __forceinline__ f32x16 mma(const f32x8& a, const f32x8& b, f32x16 c) 
   return c;
 }
 
-// LDS tile of KB rows of DH elements in 16-byte chunks, the chunk index XOR-swizzled by
+// LDS tile of rows of DH elements in 16-byte chunks, the chunk index XOR-swizzled by
 // the row: sixteen rows read at one chunk, and four rows read at four neighbouring
 // chunks (the transposing reads), fall on different banks.
 template <typename T, int DH>
 struct Tile {
   static constexpr int VE = Elem<T>::VE, NC = DH / VE;   // chunks of a row
-  static constexpr int ELEMS = KB * DH;
   __device__ static __forceinline__ int at(int row, int chunk) {
     const int f = NC >= 16 ? ((row & 3) << 2) | ((row >> 2) & 3)
                            : (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
@@ -82,20 +81,33 @@ struct Tile {
   }
 };
 
-// KB rows starting at row0 (rows past `last` read as row `last`), columns past dh zero.
-template <typename T, int DH, int NT>
-__device__ __forceinline__ void stage(T* lds, const T* __restrict__ g, long ld, int row0, int last,
-                                      int dh, int tid) {
+// A block of KB rows (of the NT threads' workgroup) on its way through registers: the next block is requested before
+// the current one's products and stored to the other LDS buffer after them.
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+template <typename T, int DH, int KB, int NT>
+struct Block {
   typedef Tile<T, DH> L;
+  static constexpr int N = KB * L::NC / NT;
+  u32x4 v[N];
+  // rows row0 .. (rows past `last` read as row `last`), columns past dh zero
+  __device__ __forceinline__ void load(const T* __restrict__ g, long ld, int row0, int last, int dh,
+                                       int tid) {
 #pragma unroll
-  for (int k = 0; k < KB * L::NC / NT; ++k) {
-    const int i = tid + NT * k, r = i / L::NC, ch = i % L::NC;
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (ch * L::VE < dh)
-      v = *reinterpret_cast<const uint4*>(g + (long)min(row0 + r, last) * ld + ch * L::VE);
-    *reinterpret_cast<uint4*>(lds + L::at(r, ch)) = v;
+    for (int k = 0; k < N; ++k) {
+      const int i = tid + NT * k, r = i / L::NC, ch = i % L::NC;
+      v[k] = u32x4{0, 0, 0, 0};
+      if (ch * L::VE < dh)
+        v[k] = *reinterpret_cast<const u32x4*>(g + (long)min(row0 + r, last) * ld + ch * L::VE);
+    }
   }
-}
+  __device__ __forceinline__ void store(T* lds, int tid) const {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int i = tid + NT * k;
+      *reinterpret_cast<u32x4*>(lds + L::at(i / L::NC, i % L::NC)) = v[k];
+    }
+  }
+};
 
 // Fragment c of a row in global memory: elements 8 NG c + 8 g .. + 7, zero past dh.
 template <int NG>
@@ -214,32 +226,37 @@ __device__ __forceinline__ void store_row(T* row, const V (&acc)[NE], float f, i
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Tile and head of this workgroup: heads vary slowest, and when the grid divides
-// evenly each XCD (workgroups go to the 8 of them round-robin) is given a contiguous
-// run, so the tiles that share keys meet in one L2.
-__device__ __forceinline__ void tile_of(int& tile, int& head) {
-  const int L = blockIdx.x + gridDim.x * blockIdx.y;
-  const int N = gridDim.x * gridDim.y;
-  const int i = (N & 7) == 0 ? (L & 7) * (N >> 3) + (L >> 3) : L;
-  head = i / gridDim.x;
-  tile = i - head * gridDim.x;
+// Rank (0 = most work) and head of this workgroup: ranks vary slowest, so the longest
+// tiles of all heads start first, and where the heads divide by 8 each XCD (workgroups
+// go to the 8 of them round-robin) has neighbouring heads, which share keys in its L2.
+__device__ __forceinline__ void tile_of(int heads, int& rank, int& head) {
+  const int L = blockIdx.x;
+  rank = L / heads;
+  const int i = L - rank * heads;
+  head = (heads & 7) == 0 ? (i & 7) * (heads >> 3) + (i >> 3) : i;
 }
 
 // ---------------------------------------------------------------- forward
-template <typename T, int DH, int R, bool DUAL>
-__global__ void __launch_bounds__(64 * PK_TILE / R) packed_fwd_kernel(PackedAttnArgs<T> a) {
-  constexpr int NT = 64 * PK_TILE / R, NG = 64 / R, NS = KB / R, NE = DH / R, NC = DH / (8 * NG);
-  constexpr int AV = R * R / 64, NK = KB / (8 * NG);
+// A workgroup owns NW R queries of one head.  Scores are formed for SB keys at a time
+// and consumed before the next SB, which bounds the registers they need.  The running
+// maximum is only raised, and the accumulators rescaled, when a score exceeds it by
+// more than 2^8: until then exp2 stays below 2^8 times its usual range, far from
+// float32's, and a factor common to numerator and denominator changes neither's
+// relative error.
+template <typename T, int DH, int R, int NW, int KB, int MW, bool DUAL>
+__global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<T> a) {
+  constexpr int NT = 64 * NW, NG = 64 / R, NS = SB / R, NE = DH / R, NC = DH / (8 * NG);
+  constexpr int AV = R * R / 64, NK = SB / (8 * NG);
   typedef typename AccT<R>::V V;
   typedef typename FragT<T>::V F;
   typedef Tile<T, DH> L;
-  __shared__ __attribute__((aligned(16))) T sK[L::ELEMS], sV[L::ELEMS], sKd[DUAL ? L::ELEMS : 8],
-      sVd[DUAL ? L::ELEMS : 8];
-  int ti, h;
-  tile_of(ti, h);
-  const int nt = a.p.head[0];
-  if (ti >= nt) return;
-  const int4 tile = a.p.tile[nt - 1 - ti];
+  __shared__ __attribute__((aligned(16))) T sK[2][KB * DH], sV[2][KB * DH],
+      sKd[DUAL ? 2 : 1][DUAL ? KB * DH : 8], sVd[DUAL ? 2 : 1][DUAL ? KB * DH : 8];
+  int rank, h;
+  tile_of(a.H, rank, h);
+  const TileList tl = a.p.list[tile_kind(NW * R)];
+  if (rank >= a.p.head[tile_kind(NW * R)]) return;
+  const int4 tile = tl.byq[rank];
   const int lo = tile.y, hi = tile.z;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, lr = lane % R, g = lane / R;
   const int q0 = tile.x + w * R, q = q0 + lr, qc = min(q, hi - 1);
@@ -262,80 +279,101 @@ __global__ void __launch_bounds__(64 * PK_TILE / R) packed_fwd_kernel(PackedAttn
     zero(o[e]);
     if constexpr (DUAL) zero(od[e]);
   }
-  const int qlast = min(tile.x + PK_TILE, hi) - 1;
-  for (int k0 = lo; k0 <= qlast; k0 += KB) {
-    __syncthreads();
-    stage<T, DH, NT>(sK, K, a.ldk, k0, hi - 1, dh, tid);
-    stage<T, DH, NT>(sV, Vp, a.ldv, k0, hi - 1, dh, tid);
+  Block<T, DH, KB, NT> rK, rV, rKd, rVd;
+  auto load = [&](int k0) {
+    rK.load(K, a.ldk, k0, hi - 1, dh, tid);
+    rV.load(Vp, a.ldv, k0, hi - 1, dh, tid);
     if constexpr (DUAL) {
-      stage<T, DH, NT>(sKd, Kd, a.ldkd, k0, hi - 1, dh, tid);
-      stage<T, DH, NT>(sVd, Vd, a.ldvd, k0, hi - 1, dh, tid);
+      rKd.load(Kd, a.ldkd, k0, hi - 1, dh, tid);
+      rVd.load(Vd, a.ldvd, k0, hi - 1, dh, tid);
     }
-    __syncthreads();
-    if (k0 > q0 + R - 1 || q0 >= hi) continue;   // nothing of the block is visible to the wave
-    V s[NS], sd[DUAL ? NS : 1];
+  };
+  auto store = [&](int b) {
+    rK.store(sK[b], tid);
+    rV.store(sV[b], tid);
+    if constexpr (DUAL) {
+      rKd.store(sKd[b], tid);
+      rVd.store(sVd[b], tid);
+    }
+  };
+  const int nb = (min(tile.x + NW * R, hi) - 1 - lo) / KB + 1;
+  load(lo);
+  store(0);
+  for (int kb = 0; kb < nb; ++kb) {
+    __syncthreads();   // block kb is in its buffer, and nobody reads the other one
+    const int k0 = lo + kb * KB, b = kb & 1;
+    if (kb + 1 < nb) load(k0 + KB);
 #pragma unroll
-    for (int n = 0; n < NS; ++n) {
-      zero(s[n]);
-      if constexpr (DUAL) zero(sd[n]);
+    for (int sb = 0; sb < KB / SB; ++sb) {
+      const int ks = k0 + sb * SB;
+      if (ks > q0 + R - 1 || q0 >= hi) break;   // nothing further is visible to the wave
+      V s[NS], sd[DUAL ? NS : 1];
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const F kf = frag<DH, NG>(sK, n * R + lr, g, c);
-        s[n] = mma(kf, qf[c], s[n]);
+      for (int n = 0; n < NS; ++n) {
+        zero(s[n]);
+        if constexpr (DUAL) zero(sd[n]);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const F kf = frag<DH, NG>(sK[b], sb * SB + n * R + lr, g, c);
+          s[n] = mma(kf, qf[c], s[n]);
+          if constexpr (DUAL) {
+            sd[n] = mma(kf, qdf[c], sd[n]);
+            sd[n] = mma(frag<DH, NG>(sKd[b], sb * SB + n * R + lr, g, c), qf[c], sd[n]);
+          }
+        }
+      }
+      if (ks + SB - 1 > q0) {   // some key may follow some query
+#pragma unroll
+        for (int t = 0; t < NS * AV; ++t)
+          if (ks + 4 * NG * (t / 4) + 4 * g + t % 4 > q) {
+            s[t / AV][t % AV] = -INFINITY;
+            if constexpr (DUAL) sd[t / AV][t % AV] = 0.f;
+          }
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < NS * AV; ++t) mx = fmaxf(mx, s[t / AV][t % AV]);
+      // the first keys hold a visible one of every query: m is finite from then on
+      mx = max_groups<R>(mx) * s2;
+      if (__any(mx > m + 8.f)) {
+        const float mn = fmaxf(m, mx), al = exp2_(m - mn);
+        m = mn;
+        l *= al;
+        if constexpr (DUAL) cs *= al;
+#pragma unroll
+        for (int e = 0; e < NE; ++e) {
+          o[e] *= al;
+          if constexpr (DUAL) od[e] *= al;
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < NS * AV; ++t) {
+        const float p = exp2_(fmaf(s[t / AV][t % AV], s2, -m));
+        s[t / AV][t % AV] = p;
+        l += p;
         if constexpr (DUAL) {
-          sd[n] = mma(kf, qdf[c], sd[n]);
-          sd[n] = mma(frag<DH, NG>(sKd, n * R + lr, g, c), qf[c], sd[n]);
+          const float pd = p * (sd[t / AV][t % AV] * a.scale);
+          sd[t / AV][t % AV] = pd;
+          cs += pd;
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < NK; ++c) {
+        F pf, pdf;
+        pack(s, c, pf);
+        if constexpr (DUAL) pack(sd, c, pdf);
+#pragma unroll
+        for (int e = 0; e < NE; ++e) {
+          const F vf = tfrag<DH, R>(sV[b], e, lane, sb * NK + c);
+          o[e] = mma(vf, pf, o[e]);
+          if constexpr (DUAL) {
+            od[e] = mma(vf, pdf, od[e]);
+            od[e] = mma(tfrag<DH, R>(sVd[b], e, lane, sb * NK + c), pf, od[e]);
+          }
         }
       }
     }
-    const bool diag = k0 + KB - 1 > q0;
-    float mx = -INFINITY;
-#pragma unroll
-    for (int t = 0; t < NS * AV; ++t) {
-      float v = s[t / AV][t % AV] * s2;
-      if (diag && k0 + 4 * NG * (t / 4) + 4 * g + t % 4 > q) v = -INFINITY;
-      s[t / AV][t % AV] = v;
-      mx = fmaxf(mx, v);
-    }
-    // block lo holds a visible key of every query, so m is finite from the first block on
-    const float mn = fmaxf(m, max_groups<R>(mx));
-    const float al = exp2_(m - mn);
-    m = mn;
-    float ls = 0.f, lc = 0.f;
-#pragma unroll
-    for (int t = 0; t < NS * AV; ++t) {
-      const float sv = s[t / AV][t % AV];
-      const float p = exp2_(sv - mn);
-      s[t / AV][t % AV] = p;
-      ls += p;
-      if constexpr (DUAL) {
-        const float pd = sv == -INFINITY ? 0.f : p * (sd[t / AV][t % AV] * a.scale);
-        sd[t / AV][t % AV] = pd;
-        lc += pd;
-      }
-    }
-    l = l * al + ls;
-    if constexpr (DUAL) cs = cs * al + lc;
-#pragma unroll
-    for (int e = 0; e < NE; ++e) {
-      o[e] *= al;
-      if constexpr (DUAL) od[e] *= al;
-    }
-#pragma unroll
-    for (int c = 0; c < NK; ++c) {
-      F pf, pdf;
-      pack(s, c, pf);
-      if constexpr (DUAL) pack(sd, c, pdf);
-#pragma unroll
-      for (int e = 0; e < NE; ++e) {
-        const F vf = tfrag<DH, R>(sV, e, lane, c);
-        o[e] = mma(vf, pf, o[e]);
-        if constexpr (DUAL) {
-          od[e] = mma(vf, pdf, od[e]);
-          od[e] = mma(tfrag<DH, R>(sVd, e, lane, c), pf, od[e]);
-        }
-      }
-    }
+    if (kb + 1 < nb) store(b ^ 1);
   }
   if (q >= hi) return;   // (lanes of one row leave together; q0 < hi has l > 0)
   const float lt = sum_groups<R>(l), inv = 1.0f / lt;
@@ -366,20 +404,21 @@ __device__ __forceinline__ float dot(const f32x8& a, const f32x8& b) {
   return s;
 }
 
-template <typename T, int DH, int R, bool DUAL>
-__global__ void __launch_bounds__(64 * PK_TILE / R) packed_dq_kernel(PackedAttnArgs<T> a) {
-  constexpr int NT = 64 * PK_TILE / R, NG = 64 / R, NS = KB / R, NE = DH / R, NC = DH / (8 * NG);
-  constexpr int AV = R * R / 64, NK = KB / (8 * NG);
+// Scores' cotangents are formed without the scale s, which the sums take at the end.
+template <typename T, int DH, int R, int NW, int KB, int MW, bool DUAL>
+__global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T> a) {
+  constexpr int NT = 64 * NW, NG = 64 / R, NS = SB / R, NE = DH / R, NC = DH / (8 * NG);
+  constexpr int AV = R * R / 64, NK = SB / (8 * NG);
   typedef typename AccT<R>::V V;
   typedef typename FragT<T>::V F;
   typedef Tile<T, DH> L;
-  __shared__ __attribute__((aligned(16))) T sK[L::ELEMS], sV[L::ELEMS], sKd[DUAL ? L::ELEMS : 8],
-      sVd[DUAL ? L::ELEMS : 8];
-  int ti, h;
-  tile_of(ti, h);
-  const int nt = a.p.head[0];
-  if (ti >= nt) return;
-  const int4 tile = a.p.tile[nt - 1 - ti];
+  __shared__ __attribute__((aligned(16))) T sK[2][KB * DH], sV[2][KB * DH],
+      sKd[DUAL ? 2 : 1][DUAL ? KB * DH : 8], sVd[DUAL ? 2 : 1][DUAL ? KB * DH : 8];
+  int rank, h;
+  tile_of(a.H, rank, h);
+  const TileList tl = a.p.list[tile_kind(NW * R)];
+  if (rank >= a.p.head[tile_kind(NW * R)]) return;
+  const int4 tile = tl.byq[rank];
   const int lo = tile.y, hi = tile.z;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, lr = lane % R, g = lane / R;
   const int q0 = tile.x + w * R, q = q0 + lr, qc = min(q, hi - 1);
@@ -418,87 +457,119 @@ __global__ void __launch_bounds__(64 * PK_TILE / R) packed_dq_kernel(PackedAttnA
     zero(dq[e]);
     if constexpr (DUAL) zero(dqd[e]);
   }
-  const int qlast = min(tile.x + PK_TILE, hi) - 1;
-  for (int k0 = lo; k0 <= qlast; k0 += KB) {
-    __syncthreads();
-    stage<T, DH, NT>(sK, K, a.ldk, k0, hi - 1, dh, tid);
-    stage<T, DH, NT>(sV, Vp, a.ldv, k0, hi - 1, dh, tid);
+  Block<T, DH, KB, NT> rK, rV, rKd, rVd;
+  auto load = [&](int k0) {
+    rK.load(K, a.ldk, k0, hi - 1, dh, tid);
+    rV.load(Vp, a.ldv, k0, hi - 1, dh, tid);
     if constexpr (DUAL) {
-      stage<T, DH, NT>(sKd, Kd, a.ldkd, k0, hi - 1, dh, tid);
-      stage<T, DH, NT>(sVd, Vd, a.ldvd, k0, hi - 1, dh, tid);
+      rKd.load(Kd, a.ldkd, k0, hi - 1, dh, tid);
+      rVd.load(Vd, a.ldvd, k0, hi - 1, dh, tid);
     }
+  };
+  auto store = [&](int b) {
+    rK.store(sK[b], tid);
+    rV.store(sV[b], tid);
+    if constexpr (DUAL) {
+      rKd.store(sKd[b], tid);
+      rVd.store(sVd[b], tid);
+    }
+  };
+  const int nb = (min(tile.x + NW * R, hi) - 1 - lo) / KB + 1;
+  load(lo);
+  store(0);
+  for (int kb = 0; kb < nb; ++kb) {
     __syncthreads();
-    if (k0 > q0 + R - 1 || q0 >= hi) continue;
-    const bool diag = k0 + KB - 1 > q0;
-    V ds[NS], dsd[DUAL ? NS : 1];
+    const int k0 = lo + kb * KB, b = kb & 1;
+    if (kb + 1 < nb) load(k0 + KB);
 #pragma unroll
-    for (int n = 0; n < NS; ++n) {
-      V s, sd, dp, dpd;
-      zero(s); zero(sd); zero(dp); zero(dpd);
+    for (int sb = 0; sb < KB / SB; ++sb) {
+      const int ks = k0 + sb * SB;
+      if (ks > q0 + R - 1 || q0 >= hi) break;
+      const bool diag = ks + SB - 1 > q0;
+      V ds[NS], dsd[DUAL ? NS : 1];
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const F kf = frag<DH, NG>(sK, n * R + lr, g, c), vf = frag<DH, NG>(sV, n * R + lr, g, c);
-        s = mma(kf, qf[c], s);
-        dp = mma(vf, gf[c], dp);
-        if constexpr (DUAL) {
-          sd = mma(kf, qdf[c], sd);
-          sd = mma(frag<DH, NG>(sKd, n * R + lr, g, c), qf[c], sd);
-          dpd = mma(vf, gdf[c], dpd);
-          dpd = mma(frag<DH, NG>(sVd, n * R + lr, g, c), gf[c], dpd);
+      for (int n = 0; n < NS; ++n) {
+        V s, sd, dp, dpd;
+        zero(s); zero(sd); zero(dp); zero(dpd);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const int kr = sb * SB + n * R + lr;
+          const F kf = frag<DH, NG>(sK[b], kr, g, c), vf = frag<DH, NG>(sV[b], kr, g, c);
+          s = mma(kf, qf[c], s);
+          dp = mma(vf, gf[c], dp);
+          if constexpr (DUAL) {
+            sd = mma(kf, qdf[c], sd);
+            sd = mma(frag<DH, NG>(sKd[b], kr, g, c), qf[c], sd);
+            dpd = mma(vf, gdf[c], dpd);
+            dpd = mma(frag<DH, NG>(sVd[b], kr, g, c), gf[c], dpd);
+          }
+        }
+#pragma unroll
+        for (int t = 0; t < AV; ++t) {
+          const float p = exp2_(fmaf(s[t], s2, -lse));
+          const float x = dp[t] - r;
+          ds[n][t] = p * x;
+          if constexpr (DUAL) {
+            const float pd = p * fmaf(sd[t], a.scale, -cst);
+            dsd[n][t] = fmaf(pd, x, p * (dpd[t] - rd));
+          }
+        }
+        if (diag) {
+#pragma unroll
+          for (int t = 0; t < AV; ++t)
+            if (ks + n * R + 4 * NG * (t / 4) + 4 * g + t % 4 > q) {
+              ds[n][t] = 0.f;
+              if constexpr (DUAL) dsd[n][t] = 0.f;
+            }
         }
       }
 #pragma unroll
-      for (int t = 0; t < AV; ++t) {
-        const bool ok = !diag || k0 + n * R + 4 * NG * (t / 4) + 4 * g + t % 4 <= q;
-        const float p = exp2_(s[t] * s2 - lse);
-        const float x = dp[t] - r;
-        ds[n][t] = ok ? a.scale * p * x : 0.f;
-        if constexpr (DUAL) {
-          const float pd = p * (sd[t] * a.scale - cst);
-          dsd[n][t] = ok ? a.scale * (pd * x + p * (dpd[t] - rd)) : 0.f;
+      for (int c = 0; c < NK; ++c) {
+        F df, ddf;
+        pack(ds, c, df);
+        if constexpr (DUAL) pack(dsd, c, ddf);
+#pragma unroll
+        for (int e = 0; e < NE; ++e) {
+          const F kt = tfrag<DH, R>(sK[b], e, lane, sb * NK + c);
+          dq[e] = mma(kt, df, dq[e]);
+          if constexpr (DUAL) {
+            dqd[e] = mma(kt, ddf, dqd[e]);
+            dqd[e] = mma(tfrag<DH, R>(sKd[b], e, lane, sb * NK + c), df, dqd[e]);
+          }
         }
       }
     }
-#pragma unroll
-    for (int c = 0; c < NK; ++c) {
-      F df, ddf;
-      pack(ds, c, df);
-      if constexpr (DUAL) pack(dsd, c, ddf);
-#pragma unroll
-      for (int e = 0; e < NE; ++e) {
-        const F kt = tfrag<DH, R>(sK, e, lane, c);
-        dq[e] = mma(kt, df, dq[e]);
-        if constexpr (DUAL) {
-          dqd[e] = mma(kt, ddf, dqd[e]);
-          dqd[e] = mma(tfrag<DH, R>(sKd, e, lane, c), df, dqd[e]);
-        }
-      }
-    }
+    if (kb + 1 < nb) store(b ^ 1);
   }
   if (q >= hi) return;
-  store_row<R, NE>(a.dq + q * a.lddq + (long)h * dh, dq, 1.f, g, dh);
-  if constexpr (DUAL) store_row<R, NE>(a.dqd + q * a.lddqd + (long)h * dh, dqd, 1.f, g, dh);
+  store_row<R, NE>(a.dq + q * a.lddq + (long)h * dh, dq, a.scale, g, dh);
+  if constexpr (DUAL) store_row<R, NE>(a.dqd + q * a.lddqd + (long)h * dh, dqd, a.scale, g, dh);
 }
 
 // ---------------------------------------------------------------- backward: dK, dV
-template <typename T, int DH, int R, bool DUAL>
-__global__ void __launch_bounds__(64 * PK_TILE / R) packed_dkv_kernel(PackedAttnArgs<T> a) {
-  constexpr int NT = 64 * PK_TILE / R, NG = 64 / R, NS = KB / R, NE = DH / R, NC = DH / (8 * NG);
-  constexpr int AV = R * R / 64, NK = KB / (8 * NG);
+// A workgroup owns NW R keys of one key head and goes through the queries of some of the
+// head's query heads (all, or one part of `parts`, whose float32 sums dkv_sum_kernel
+// adds in order).
+template <typename T, int DH, int R, int NW, int KB, int MW, bool DUAL>
+__global__ void __launch_bounds__(64 * NW, MW) packed_dkv_kernel(PackedAttnArgs<T> a) {
+  constexpr int NT = 64 * NW, NG = 64 / R, NS = SB / R, NE = DH / R, NC = DH / (8 * NG);
+  constexpr int AV = R * R / 64, NK = SB / (8 * NG);
   typedef typename AccT<R>::V V;
   typedef typename FragT<T>::V F;
   typedef Tile<T, DH> L;
-  __shared__ __attribute__((aligned(16))) T sQ[L::ELEMS], sG[L::ELEMS], sQd[DUAL ? L::ELEMS : 8],
-      sGd[DUAL ? L::ELEMS : 8];
-  __shared__ __attribute__((aligned(16))) float sL[KB], sR[KB], sC[KB], sRd[KB];
-  int ti, kh;
-  tile_of(ti, kh);
-  if (ti >= a.p.head[0]) return;
-  const int4 tile = a.p.tile[ti];
-  const int hi = tile.z;
+  __shared__ __attribute__((aligned(16))) T sQ[2][KB * DH], sG[2][KB * DH],
+      sQd[DUAL ? 2 : 1][DUAL ? KB * DH : 8], sGd[DUAL ? 2 : 1][DUAL ? KB * DH : 8];
+  __shared__ __attribute__((aligned(16))) float sL[2][KB], sR[2][KB], sC[2][KB], sRd[2][KB];
+  int rank, hp;
+  tile_of(a.K * a.parts, rank, hp);
+  const TileList tl = a.p.list[tile_kind(NW * R)];
+  if (rank >= a.p.head[tile_kind(NW * R)]) return;
+  const int4 tile = tl.byk[rank];
+  const int kh = hp / a.parts, part = hp - kh * a.parts, hi = tile.z;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, lr = lane % R, g = lane / R;
   const int k0 = tile.x + w * R, k = k0 + lr, kc = min(k, hi - 1);
-  const int G = a.H / a.K, dh = a.dh;
+  const int GP = a.H / a.K / a.parts, dh = a.dh;   // query heads of a part
+  const int h0 = (kh * a.parts + part) * GP;
   F kf[NC], vf[NC], kdf[DUAL ? NC : 1], vdf[DUAL ? NC : 1];
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
@@ -520,31 +591,53 @@ __global__ void __launch_bounds__(64 * PK_TILE / R) packed_dkv_kernel(PackedAttn
       zero(dvd[e]);
     }
   }
-  for (int h = kh * G; h < (kh + 1) * G; ++h) {
-    const T* Q = a.q + (long)h * dh;
-    const T* Gp = a.g + (long)h * dh;
-    const T* Qd = DUAL ? a.qd + (long)h * dh : nullptr;
-    const T* Gd = DUAL ? a.gd + (long)h * dh : nullptr;
-    for (int q0 = tile.x; q0 < hi; q0 += KB) {
-      __syncthreads();
-      stage<T, DH, NT>(sQ, Q, a.ldq, q0, hi - 1, dh, tid);
-      stage<T, DH, NT>(sG, Gp, a.ldg, q0, hi - 1, dh, tid);
+  Block<T, DH, KB, NT> rQ, rG, rQd, rGd;
+  float xL = 0.f, xR = 0.f, xC = 0.f, xRd = 0.f;   // a query's row values (threads 0 .. 63)
+  const int nq = (hi - tile.x + KB - 1) / KB, nb = nq * GP;
+  auto load = [&](int i) {   // block i: query head i / nq, its block i % nq
+    const int hq = i / nq, h = h0 + hq, r0 = tile.x + (i - hq * nq) * KB;
+    rQ.load(a.q + (long)h * dh, a.ldq, r0, hi - 1, dh, tid);
+    rG.load(a.g + (long)h * dh, a.ldg, r0, hi - 1, dh, tid);
+    if constexpr (DUAL) {
+      rQd.load(a.qd + (long)h * dh, a.ldqd, r0, hi - 1, dh, tid);
+      rGd.load(a.gd + (long)h * dh, a.ldgd, r0, hi - 1, dh, tid);
+    }
+    const long x = (long)h * a.p.n + min(r0 + (tid & (KB - 1)), hi - 1);
+    xL = a.lse[x];
+    xR = a.r[x];
+    if constexpr (DUAL) {
+      xC = a.cst[x];
+      xRd = a.rd[x];
+    }
+  };
+  auto store = [&](int b) {
+    rQ.store(sQ[b], tid);
+    rG.store(sG[b], tid);
+    if constexpr (DUAL) {
+      rQd.store(sQd[b], tid);
+      rGd.store(sGd[b], tid);
+    }
+    if (tid < KB) {
+      sL[b][tid] = xL;
+      sR[b][tid] = xR;
       if constexpr (DUAL) {
-        stage<T, DH, NT>(sQd, Qd, a.ldqd, q0, hi - 1, dh, tid);
-        stage<T, DH, NT>(sGd, Gd, a.ldgd, q0, hi - 1, dh, tid);
+        sC[b][tid] = xC;
+        sRd[b][tid] = xRd;
       }
-      if (tid < KB) {
-        const long i = (long)h * a.p.n + min(q0 + tid, hi - 1);
-        sL[tid] = a.lse[i];
-        sR[tid] = a.r[i];
-        if constexpr (DUAL) {
-          sC[tid] = a.cst[i];
-          sRd[tid] = a.rd[i];
-        }
-      }
-      __syncthreads();
-      if (q0 + KB - 1 < k0 || k0 >= hi) continue;   // every query of the block precedes the wave's keys
-      const bool mask = q0 < k0 + R - 1 || q0 + KB > hi;
+    }
+  };
+  load(0);
+  store(0);
+  int r0 = tile.x;   // first query of the block
+  for (int i = 0; i < nb; ++i) {
+    __syncthreads();
+    const int b = i & 1;
+    if (i + 1 < nb) load(i + 1);
+#pragma unroll
+    for (int sb = 0; sb < KB / SB; ++sb) {
+      const int qs = r0 + sb * SB;
+      if (qs + SB - 1 < k0 || k0 >= hi || qs >= hi) continue;   // no query of these sees the wave's keys
+      const bool mask = qs < k0 + R - 1 || qs + SB > hi;
       V p[NS], ds[NS], pd[DUAL ? NS : 1], dsd[DUAL ? NS : 1];
 #pragma unroll
       for (int n = 0; n < NS; ++n) {
@@ -552,28 +645,44 @@ __global__ void __launch_bounds__(64 * PK_TILE / R) packed_dkv_kernel(PackedAttn
         zero(s); zero(sd); zero(dp); zero(dpd);
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-          const F qq = frag<DH, NG>(sQ, n * R + lr, g, c), gg = frag<DH, NG>(sG, n * R + lr, g, c);
+          const int qr = sb * SB + n * R + lr;
+          const F qq = frag<DH, NG>(sQ[b], qr, g, c), gg = frag<DH, NG>(sG[b], qr, g, c);
           s = mma(qq, kf[c], s);
           dp = mma(gg, vf[c], dp);
           if constexpr (DUAL) {
             sd = mma(qq, kdf[c], sd);
-            sd = mma(frag<DH, NG>(sQd, n * R + lr, g, c), kf[c], sd);
+            sd = mma(frag<DH, NG>(sQd[b], qr, g, c), kf[c], sd);
             dpd = mma(gg, vdf[c], dpd);
-            dpd = mma(frag<DH, NG>(sGd, n * R + lr, g, c), vf[c], dpd);
+            dpd = mma(frag<DH, NG>(sGd[b], qr, g, c), vf[c], dpd);
           }
         }
 #pragma unroll
-        for (int t = 0; t < AV; ++t) {
-          const int i = n * R + 4 * NG * (t / 4) + 4 * g + t % 4;
-          const bool ok = !mask || (q0 + i >= k && q0 + i < hi);
-          const float pv = ok ? exp2_(s[t] * s2 - sL[i]) : 0.f;
-          const float x = dp[t] - sR[i];
-          p[n][t] = pv;
-          ds[n][t] = ok ? a.scale * pv * x : 0.f;
+        for (int t4 = 0; t4 < AV; t4 += 4) {
+          const int i4 = sb * SB + n * R + NG * t4 + 4 * g;   // four queries of the block
+          const f32x4 Lq = *reinterpret_cast<const f32x4*>(&sL[b][i4]);
+          const f32x4 Rq = *reinterpret_cast<const f32x4*>(&sR[b][i4]);
+          f32x4 Cq, Dq;
           if constexpr (DUAL) {
-            const float pdv = ok ? pv * (sd[t] * a.scale - sC[i]) : 0.f;
-            pd[n][t] = pdv;
-            dsd[n][t] = ok ? a.scale * (pdv * x + pv * (dpd[t] - sRd[i])) : 0.f;
+            Cq = *reinterpret_cast<const f32x4*>(&sC[b][i4]);
+            Dq = *reinterpret_cast<const f32x4*>(&sRd[b][i4]);
+          }
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int t = t4 + u;
+            float pv = exp2_(fmaf(s[t], s2, -Lq[u]));
+            float x = dp[t] - Rq[u], y = 0.f, z = 0.f;
+            if constexpr (DUAL) {
+              y = fmaf(sd[t], a.scale, -Cq[u]);
+              z = dpd[t] - Dq[u];
+            }
+            if (mask && !(r0 + i4 + u >= k && r0 + i4 + u < hi)) pv = x = y = z = 0.f;
+            p[n][t] = pv;
+            ds[n][t] = pv * x;
+            if constexpr (DUAL) {
+              const float pdv = pv * y;
+              pd[n][t] = pdv;
+              dsd[n][t] = fmaf(pdv, x, pv * z);
+            }
           }
         }
       }
@@ -588,78 +697,114 @@ __global__ void __launch_bounds__(64 * PK_TILE / R) packed_dkv_kernel(PackedAttn
         }
 #pragma unroll
         for (int e = 0; e < NE; ++e) {
-          const F gt = tfrag<DH, R>(sG, e, lane, c), qt = tfrag<DH, R>(sQ, e, lane, c);
+          const F gt = tfrag<DH, R>(sG[b], e, lane, sb * NK + c);
+          const F qt = tfrag<DH, R>(sQ[b], e, lane, sb * NK + c);
           dv[e] = mma(gt, pf, dv[e]);
           dk[e] = mma(qt, df, dk[e]);
           if constexpr (DUAL) {
             dvd[e] = mma(gt, pdf, dvd[e]);
-            dvd[e] = mma(tfrag<DH, R>(sGd, e, lane, c), pf, dvd[e]);
+            dvd[e] = mma(tfrag<DH, R>(sGd[b], e, lane, sb * NK + c), pf, dvd[e]);
             dkd[e] = mma(qt, ddf, dkd[e]);
-            dkd[e] = mma(tfrag<DH, R>(sQd, e, lane, c), df, dkd[e]);
+            dkd[e] = mma(tfrag<DH, R>(sQd[b], e, lane, sb * NK + c), df, dkd[e]);
           }
         }
       }
     }
+    r0 += KB;
+    if (r0 >= hi) r0 = tile.x;
+    if (i + 1 < nb) store(b ^ 1);
   }
   if (k >= hi) return;
-  store_row<R, NE>(a.dk + k * a.lddk + (long)kh * dh, dk, 1.f, g, dh);
+  if (a.parts > 1) {
+    float* P = a.partial + (((long)part * a.p.n + k) * a.K + kh) * (DUAL ? 4 : 2) * dh;
+    store_row<R, NE>(P, dk, a.scale, g, dh);
+    store_row<R, NE>(P + dh, dv, 1.f, g, dh);
+    if constexpr (DUAL) {
+      store_row<R, NE>(P + 2 * dh, dkd, a.scale, g, dh);
+      store_row<R, NE>(P + 3 * dh, dvd, 1.f, g, dh);
+    }
+    return;
+  }
+  store_row<R, NE>(a.dk + k * a.lddk + (long)kh * dh, dk, a.scale, g, dh);
   store_row<R, NE>(a.dv + k * a.lddv + (long)kh * dh, dv, 1.f, g, dh);
   if constexpr (DUAL) {
-    store_row<R, NE>(a.dkd + k * a.lddkd + (long)kh * dh, dkd, 1.f, g, dh);
+    store_row<R, NE>(a.dkd + k * a.lddkd + (long)kh * dh, dkd, a.scale, g, dh);
     store_row<R, NE>(a.dvd + k * a.lddvd + (long)kh * dh, dvd, 1.f, g, dh);
   }
 }
 
+// dK, dV (and tangents) as the sums of their parts, four dims a thread.
+template <typename T>
+__global__ void __launch_bounds__(256) dkv_sum_kernel(PackedAttnArgs<T> a) {
+  const int na = a.dual ? 4 : 2, d4 = a.dh / 4;
+  const long i = (long)blockIdx.x * 256 + threadIdx.x;
+  const int per = a.K * na * d4;   // fours of a token
+  const long tok = i / per;
+  if (tok < a.p.head[2] || tok >= a.p.head[3]) return;
+  const int j = (int)(i - tok * per), d = 4 * (j % d4), k = j / d4 % na, kh = j / d4 / na;
+  const float* P = a.partial + ((tok * a.K + kh) * na + k) * a.dh + d;
+  f32x4 s = *reinterpret_cast<const f32x4*>(P);
+  for (int p = 1; p < a.parts; ++p)
+    s += *reinterpret_cast<const f32x4*>(P + (long)p * a.p.n * a.K * na * a.dh);
+  T* out = k == 0 ? a.dk + tok * a.lddk : k == 1 ? a.dv + tok * a.lddv
+         : k == 2 ? a.dkd + tok * a.lddkd : a.dvd + tok * a.lddvd;
+  store4(out + (long)kh * a.dh + d, s[0], s[1], s[2], s[3]);
+}
+
 // ---------------------------------------------------------------- plan
-// Bounds made ascending (running maximum of the clamped offsets) and the tiles before
-// each sequence, by one workgroup over chunks of its size.
+// Bounds made ascending (running maximum of the clamped offsets) and, for both tile
+// sizes, the tiles before each sequence, by one workgroup over chunks of its size.
 constexpr int SCAN = 1024;
 __global__ void __launch_bounds__(SCAN) plan_scan_kernel(SeqPlanArgs a) {
-  __shared__ int sv[SCAN], carry[2];
+  __shared__ int sv[SCAN], carry;
   const int tid = threadIdx.x, m = a.p.m, n = (int)a.p.n;
   auto raw = [&](int j) {
     if (!a.cu) return (int)min((long)j * a.len, (long)n);
     if (!a.cover) return min(max(a.cu[j], 0), n);
     return j == 0 ? 0 : j == m ? n : min(max(a.cu[j - 1], 0), n);
   };
-  if (tid == 0) carry[0] = carry[1] = 0;
-  __syncthreads();
+  if (tid == 0) carry = 0;
   for (int j0 = 0; j0 <= m; j0 += SCAN) {
     const int j = j0 + tid;
-    sv[tid] = j <= m ? raw(j) : 0;
     __syncthreads();
+    sv[tid] = j <= m ? raw(j) : 0;
     for (int o = 1; o < SCAN; o <<= 1) {
+      __syncthreads();
       const int x = tid >= o ? sv[tid - o] : 0;
       __syncthreads();
       sv[tid] = max(sv[tid], x);
-      __syncthreads();
     }
-    if (j <= m) a.p.bound[j] = max(sv[tid], carry[0]);
     __syncthreads();
-    if (tid == 0) carry[0] = max(carry[0], sv[SCAN - 1]);
+    if (j <= m) a.p.bound[j] = max(sv[tid], carry);
     __syncthreads();
+    if (tid == 0) carry = max(carry, sv[SCAN - 1]);
   }
-  for (int j0 = 0; j0 <= m; j0 += SCAN) {
-    const int j = j0 + tid;
-    const int t = j < m ? (a.p.bound[j + 1] - a.p.bound[j] + PK_TILE - 1) / PK_TILE : 0;
-    sv[tid] = t;
+  for (int kind = 0; kind < 2; ++kind) {
+    const int rows = tile_rows(kind);
     __syncthreads();
-    for (int o = 1; o < SCAN; o <<= 1) {
-      const int x = tid >= o ? sv[tid - o] : 0;
+    if (tid == 0) carry = 0;
+    for (int j0 = 0; j0 <= m; j0 += SCAN) {
+      const int j = j0 + tid;
       __syncthreads();
-      sv[tid] += x;
+      const int t = j < m ? (a.p.bound[j + 1] - a.p.bound[j] + rows - 1) / rows : 0;
+      sv[tid] = t;
+      for (int o = 1; o < SCAN; o <<= 1) {
+        __syncthreads();
+        const int x = tid >= o ? sv[tid - o] : 0;
+        __syncthreads();
+        sv[tid] += x;
+      }
       __syncthreads();
+      if (j <= m) a.p.list[kind].tstart[j] = carry + sv[tid] - t;
+      __syncthreads();
+      if (tid == 0) carry += sv[SCAN - 1];
     }
-    if (j <= m) a.p.tstart[j] = carry[1] + sv[tid] - t;
     __syncthreads();
-    if (tid == 0) carry[1] += sv[SCAN - 1];
-    __syncthreads();
+    if (tid == 0) a.p.head[kind] = carry;
   }
   if (tid == 0) {
-    a.p.head[0] = carry[1];
-    a.p.head[1] = a.p.bound[0];
-    a.p.head[2] = a.p.bound[m];
-    a.p.head[3] = 0;
+    a.p.head[2] = a.p.bound[0];
+    a.p.head[3] = a.p.bound[m];
   }
 }
 
@@ -673,43 +818,102 @@ __device__ __forceinline__ int last_le(const int* x, int m, int v) {
   return lo;
 }
 
-__global__ void __launch_bounds__(256) plan_fill_kernel(SeqPlanArgs a) {
-  const long i = (long)blockIdx.x * 256 + threadIdx.x;
-  const int m = a.p.m;
-  if (i < a.p.head[0]) {
-    const int j = last_le(a.p.tstart, m, (int)i);
-    a.p.tile[i] = make_int4(a.p.bound[j] + ((int)i - a.p.tstart[j]) * PK_TILE, a.p.bound[j],
-                            a.p.bound[j + 1], 0);
-  }
-  if (i < a.p.n) {
+// Workgroups 0 .. 3 write the tile lists (two sizes, by the keys a query tile sees and by
+// the queries that see a key tile), longest first, by counting into SCAN classes of
+// length; the order inside a class is free, since every tile's results are its own.
+// The others write the positions.
+constexpr int PLAN_LISTS = 4;
+__global__ void __launch_bounds__(SCAN) plan_fill_kernel(SeqPlanArgs a) {
+  const int m = a.p.m, tid = threadIdx.x;
+  if (blockIdx.x >= PLAN_LISTS) {
+    const long i = (long)(blockIdx.x - PLAN_LISTS) * SCAN + tid;
+    if (i >= a.p.n) return;
     int pos = 0;
     if (a.positions)
       pos = a.positions[i];
     else if (i >= a.p.bound[0] && i < a.p.bound[m])
       pos = (int)i - a.p.bound[last_le(a.p.bound, m, (int)i)];
     a.p.pos[i] = pos;
+    return;
+  }
+  __shared__ int count[SCAN], longest;
+  const int kind = blockIdx.x & 1, byk = blockIdx.x >> 1, rows = tile_rows(kind);
+  const TileList l = a.p.list[kind];
+  const int nt = a.p.head[kind];
+  count[tid] = 0;
+  if (tid == 0) longest = 1;
+  __syncthreads();
+  auto length = [&](int i, int4& t) {   // tiles i's rows meet
+    const int j = last_le(l.tstart, m, i), k = i - l.tstart[j], lo = a.p.bound[j], hi = a.p.bound[j + 1];
+    t = make_int4(lo + k * rows, lo, hi, 0);
+    return byk ? (hi - lo + rows - 1) / rows - k : k + 1;
+  };
+  int4 t;
+  for (int i = tid; i < nt; i += SCAN) atomicMax(&longest, length(i, t));
+  __syncthreads();
+  const int step = longest / SCAN + 1;
+  for (int i = tid; i < nt; i += SCAN) atomicAdd(&count[SCAN - 1 - length(i, t) / step], 1);
+  __syncthreads();
+  const int own = count[tid];
+  for (int o = 1; o < SCAN; o <<= 1) {
+    const int x = tid >= o ? count[tid - o] : 0;
+    __syncthreads();
+    count[tid] += x;
+    __syncthreads();
+  }
+  const int before = count[tid] - own;
+  __syncthreads();
+  count[tid] = before;
+  __syncthreads();
+  int4* out = byk ? l.byk : l.byq;
+  for (int i = tid; i < nt; i += SCAN) {
+    const int c = SCAN - 1 - length(i, t) / step;
+    out[atomicAdd(&count[c], 1)] = t;
   }
 }
 
-// Rows a wave owns: 32 where the accumulators of the pass leave a wave its registers.
-template <typename T, int DH, bool DUAL>
-constexpr int rows_of() { return sizeof(T) == 2 && !DUAL ? 32 : 16; }
+// Parts the query heads of a key head are split into for the dK/dV pass: while there are
+// too few key tiles to fill the chip.
+int dkv_parts(long n, int H, int K) {
+  const int G = H / K;
+  const long tiles = n / 128 + 1;
+  for (int p = 1; p < G; ++p)
+    if (G % p == 0 && tiles * K * p >= 1024) return p;
+  return G;
+}
+
+// Rows a wave owns, waves of a workgroup, rows of a staged block, waves a SIMD holds.
+enum Pass { FWD, DQ, DKV };
+template <typename T, int DH, bool DUAL, int PASS>
+struct Shape {
+  static constexpr bool F32 = sizeof(T) == 4, WIDE = !F32 && !DUAL && PASS != DKV;
+  static constexpr int R = WIDE ? 32 : 16;
+  static constexpr int NW = !F32 && DUAL && DH == 64 ? 8 : 4;
+  static constexpr int KB = (F32 && DH == 128 && DUAL) || (!F32 && DUAL && DH == 128 && PASS != DKV) ? 32 : 64;
+  static constexpr int MW = F32 || (DUAL && DH == 128 && PASS == DKV) ? 1 : 2;
+};
 
 template <typename T, int DH, bool DUAL>
 void launch_fwd(const PackedAttnArgs<T>& a, hipStream_t s) {
-  constexpr int R = rows_of<T, DH, DUAL>();
-  hipLaunchKernelGGL((packed_fwd_kernel<T, DH, R, DUAL>), dim3(a.p.max_tiles, a.H),
-                     dim3(64 * PK_TILE / R), 0, s, a);
+  typedef Shape<T, DH, DUAL, FWD> S;
+  hipLaunchKernelGGL((packed_fwd_kernel<T, DH, S::R, S::NW, S::KB, S::MW, DUAL>),
+                     dim3(a.p.max_tiles[tile_kind(S::R * S::NW)] * a.H), dim3(64 * S::NW), 0, s, a);
 }
 template <typename T, int DH, bool DUAL>
 hipError_t launch_bwd(const PackedAttnArgs<T>& a, hipStream_t s) {
-  constexpr int R = rows_of<T, DH, DUAL>();
-  hipLaunchKernelGGL((packed_dq_kernel<T, DH, R, DUAL>), dim3(a.p.max_tiles, a.H),
-                     dim3(64 * PK_TILE / R), 0, s, a);
+  typedef Shape<T, DH, DUAL, DQ> Q;
+  typedef Shape<T, DH, DUAL, DKV> S;
+  hipLaunchKernelGGL((packed_dq_kernel<T, DH, Q::R, Q::NW, Q::KB, Q::MW, DUAL>),
+                     dim3(a.p.max_tiles[tile_kind(Q::R * Q::NW)] * a.H), dim3(64 * Q::NW), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((packed_dkv_kernel<T, DH, R, DUAL>), dim3(a.p.max_tiles, a.K),
-                     dim3(64 * PK_TILE / R), 0, s, a);
+  hipLaunchKernelGGL((packed_dkv_kernel<T, DH, S::R, S::NW, S::KB, S::MW, DUAL>),
+                     dim3(a.p.max_tiles[tile_kind(S::R * S::NW)] * a.K * a.parts), dim3(64 * S::NW),
+                     0, s, a);
+  e = hipGetLastError();
+  if (e != hipSuccess || a.parts == 1) return e;
+  const long fours = a.p.n * a.K * (a.dual ? 4 : 2) * (a.dh / 4);
+  hipLaunchKernelGGL(dkv_sum_kernel<T>, dim3((unsigned)((fours + 255) / 256)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
@@ -731,12 +935,15 @@ SeqPlan seq_plan_at(char* base, long n, int m, size_t* bytes) {
   };
   p.n = n;
   p.m = m;
-  p.max_tiles = (int)(n / PK_TILE + std::min((long)m, n));
   p.head = (int*)take(16);
   p.bound = (int*)take(4 * ((size_t)m + 1));
-  p.tstart = (int*)take(4 * ((size_t)m + 1));
-  p.tile = (int4*)take(16 * (size_t)p.max_tiles);
   p.pos = (int*)take(4 * (size_t)n);
+  for (int k = 0; k < 2; ++k) {
+    p.max_tiles[k] = (int)(n / tile_rows(k) + std::min((long)m, n));
+    p.list[k].tstart = (int*)take(4 * ((size_t)m + 1));
+    p.list[k].byq = (int4*)take(16 * (size_t)p.max_tiles[k]);
+    p.list[k].byk = (int4*)take(16 * (size_t)p.max_tiles[k]);
+  }
   if (bytes) *bytes = off;
   return p;
 }
@@ -746,15 +953,27 @@ hipError_t seq_plan_make(const SeqPlanArgs& a, hipStream_t s) {
   hipLaunchKernelGGL(plan_scan_kernel, dim3(1), dim3(SCAN), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const long items = std::max((long)a.p.max_tiles, a.p.n);
-  hipLaunchKernelGGL(plan_fill_kernel, dim3((unsigned)((items + 255) / 256)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL(plan_fill_kernel, dim3((unsigned)(PLAN_LISTS + (a.p.n + SCAN - 1) / SCAN)),
+                     dim3(SCAN), 0, s, a);
   return hipGetLastError();
+}
+
+size_t packed_attn_ws_floats(long n, int H, int K, int dh) {
+  const int parts = dkv_parts(n, H, K);
+  return 2 * (size_t)H * n + (parts > 1 ? (size_t)parts * n * K * 4 * dh : 0);
+}
+template <typename T>
+void packed_attn_ws(PackedAttnArgs<T>& a, float* ws) {
+  a.r = ws;
+  a.rd = ws + (long)a.H * a.p.n;
+  a.parts = dkv_parts(a.p.n, a.H, a.K);
+  a.partial = a.rd + (long)a.H * a.p.n;
 }
 
 template <typename T>
 hipError_t packed_attn_fwd(const PackedAttnArgs<T>& a, hipStream_t s) {
   if (!shapes_ok(a)) return hipErrorInvalidValue;
-  if (a.p.max_tiles < 1) return hipSuccess;
+  if (a.p.n < 1 || a.p.max_tiles[0] < 1) return hipSuccess;
   if (a.dh <= 64) {
     if (a.dual) launch_fwd<T, 64, true>(a, s); else launch_fwd<T, 64, false>(a, s);
   } else {
@@ -766,7 +985,7 @@ hipError_t packed_attn_fwd(const PackedAttnArgs<T>& a, hipStream_t s) {
 template <typename T>
 hipError_t packed_attn_bwd(const PackedAttnArgs<T>& a, hipStream_t s) {
   if (!shapes_ok(a)) return hipErrorInvalidValue;
-  if (a.p.max_tiles < 1) return hipSuccess;
+  if (a.p.n < 1 || a.p.max_tiles[0] < 1) return hipSuccess;
   if (a.dh <= 64) return a.dual ? launch_bwd<T, 64, true>(a, s) : launch_bwd<T, 64, false>(a, s);
   return a.dual ? launch_bwd<T, 128, true>(a, s) : launch_bwd<T, 128, false>(a, s);
 }
@@ -775,5 +994,8 @@ template hipError_t packed_attn_fwd<bf16_t>(const PackedAttnArgs<bf16_t>&, hipSt
 template hipError_t packed_attn_fwd<float>(const PackedAttnArgs<float>&, hipStream_t);
 template hipError_t packed_attn_bwd<bf16_t>(const PackedAttnArgs<bf16_t>&, hipStream_t);
 template hipError_t packed_attn_bwd<float>(const PackedAttnArgs<float>&, hipStream_t);
+
+template void packed_attn_ws<bf16_t>(PackedAttnArgs<bf16_t>&, float*);
+template void packed_attn_ws<float>(PackedAttnArgs<float>&, float*);
 
 }  // namespace mfmg

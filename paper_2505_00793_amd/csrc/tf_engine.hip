@@ -356,7 +356,13 @@ void carve_act_bufs(const Lay& y, Carver& c, Act<T>& a, int sets, bool all) {
   if (y.fused) {
     a.S32 = a.Sd32 = a.dS32 = a.dSd32 = nullptr;
     a.dS = a.dST = a.dSd = a.dSdT = nullptr;
-    a.ar = F32(BH * S); a.ard = F32(BH * S);
+    if (y.pk) {   // (parts do not grow steadily with the rows)
+      a.ar = F32((long)std::max(packed_attn_ws_floats((long)y.Bt * S, y.H, y.K, y.dh),
+                                packed_attn_ws_floats((long)y.Bv * S, y.H, y.K, y.dh)));
+      a.ard = nullptr;
+    } else {
+      a.ar = F32(BH * S); a.ard = F32(BH * S);
+    }
   } else {
     a.S32 = F32(BH * S * S); a.Sd32 = F32(BH * S * S);
     a.dS32 = F32(BH * S * S); a.dSd32 = F32(BH * S * S);
@@ -592,10 +598,11 @@ struct TfEng {
     t.ldq = t.ldk = t.ldv = t.ldqd = t.ldkd = t.ldvd = ld;
     t.lddq = t.lddk = t.lddv = t.lddqd = t.lddkd = t.lddvd = ld;
     t.ldo = t.ldod = t.ldg = t.ldgd = y.ld(y.d);
-    t.lse = a.lse[b]; t.cst = a.cst[b]; t.r = a.ar; t.rd = a.ard;
+    t.lse = a.lse[b]; t.cst = a.cst[b];
     t.p = plan_of(Bn, val, a);
     t.H = y.H; t.K = y.K; t.dh = y.dh; t.dual = dual;
     t.scale = 1.0f / std::sqrt((float)y.dh);
+    packed_attn_ws(t, a.ar);
     return t;
   }
   // Transposed copies (where the plan has them) of operand rows the packed operators
