@@ -328,8 +328,8 @@ mfmg_status mfmg_meta_grad_noalloc(mfmg_problem_t problem, const float* theta0,
  * Rows are by token: row i of an array holds the values of token i, its heads side
  * by side (head h at columns h * head_dim).  A QKV row is q heads | k heads | v
  * heads, (heads + 2 kv_heads) * head_dim columns; query head h reads key head
- * h / (heads / kv_heads).  Leading dimensions count elements; row pointers and rows
- * must be 16-byte aligned.  T is the operand type: bfloat16 (MFMG_PREC_BF16) or
+ * h / (heads / kv_heads).  Leading dimensions count elements and are at most 2^22;
+ * row pointers and rows must be 16-byte aligned.  T is the operand type: bfloat16 (MFMG_PREC_BF16) or
  * float32; gains and the rows that enter the rotation are float32, sums are float32.
  * Tangents (names ending in d, and xd / dxd structs) are given together or not at
  * all: with them a call also returns the derivative of its outputs along them.

@@ -947,9 +947,9 @@ mfmg_status check_attn(const mfmg_attn* a, const void* plan, int64_t n, int m) {
 mfmg_status check_rows(const char* name, const void* p, int64_t ld, int64_t cols, int size) {
   if (!p) return fail(MFMG_ERR_INVALID_ARGUMENT, "null %s", name);
   if (!aligned(p, 16)) return fail(MFMG_ERR_INVALID_ARGUMENT, "%s not 16-byte aligned", name);
-  if (ld < cols || ld > (1LL << 31) || ld * size % 16)
+  if (ld < cols || ld > (1LL << 22) || ld * size % 16)
     return fail(MFMG_ERR_INVALID_ARGUMENT,
-                "%s: leading dimension %lld, needs at least %lld and rows of whole 16 bytes", name,
+                "%s: leading dimension %lld, needs %lld .. 2^22 and rows of whole 16 bytes", name,
                 (long long)ld, (long long)cols);
   return MFMG_OK;
 }

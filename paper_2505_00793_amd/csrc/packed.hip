@@ -31,6 +31,7 @@
 #include "packed.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace mfmg {
 
@@ -68,43 +69,63 @@ __device__ __forceinline__ f32x16 mma(const f32x8& a, const f32x8& b, f32x16 c) 
   return c;
 }
 
-// LDS tile of rows of DH elements in 16-byte chunks, the chunk index XOR-swizzled by
-// the row: sixteen rows read at one chunk, and four rows read at four neighbouring
-// chunks (the transposing reads), fall on different banks.
+// LDS tile of rows of DH elements in 16-byte chunks, the chunk index XOR-swizzled by the
+// row.  A fragment read's 16-byte lanes are served in sets of 0-3, 12-15, 20-23, 24-27 (and
+// so on): both with 16 rows at two neighbouring chunks and with 32 rows at one, their
+// 16 addresses cover all 64 banks; so do the 32 lanes of a transposing read (8 rows of
+// two chunks, or 4 rows of four), and for float32 the four rows of a column read.
+// (SQ_LDS_BANK_CONFLICT 0; with row bits 2 and 3 unmixed 42% of the LDS cycles of
+// 64-dim tiles were conflicts.)
 template <typename T, int DH>
 struct Tile {
   static constexpr int VE = Elem<T>::VE, NC = DH / VE;   // chunks of a row
   __device__ static __forceinline__ int at(int row, int chunk) {
-    const int f = NC >= 16 ? ((row & 3) << 2) | ((row >> 2) & 3)
-                           : (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+    const int x = (row >> 2) & 3, h = ((x ^ (x >> 1)) & 1) << 1 | x >> 1;   // 0, 2, 3, 1
+    const int f = sizeof(T) == 4 ? row & 15 : NC >= 16 ? (row & 3) << 2 | h : ((row >> 1) & 1) << 2 | h;
     return row * DH + ((chunk ^ f) * VE);
   }
 };
 
-// A block of KB rows (of the NT threads' workgroup) on its way through registers: the next block is requested before
-// the current one's products and stored to the other LDS buffer after them.
+// A block of KB rows (of the NT threads' workgroup) on its way through registers: the next
+// block is requested before the current one's products and stored to the other LDS
+// buffer after them.  A thread's chunks are NT / (chunks of a row) rows apart, so one
+// 32-bit offset serves them all (leading dimensions are below 2^22).  Columns past dh
+// repeat the row's last chunk: the other operand holds zeros there, or the results of
+// those columns are not stored.
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 template <typename T, int DH, int KB, int NT>
 struct Block {
   typedef Tile<T, DH> L;
-  static constexpr int N = KB * L::NC / NT;
+  static constexpr int N = KB * L::NC / NT, STEP = NT / L::NC;
+  static_assert(KB * L::NC % NT == 0 && NT % L::NC == 0, "chunks of a thread");
   u32x4 v[N];
-  // rows row0 .. (rows past `last` read as row `last`), columns past dh zero
-  __device__ __forceinline__ void load(const T* __restrict__ g, long ld, int row0, int last, int dh,
-                                       int tid) {
+  unsigned off;   // byte offset of the thread's chunk in the block's first STEP rows
+  unsigned ldb;
+  __device__ __forceinline__ void init(long ld, int dh, int tid) {
+    ldb = (unsigned)ld * sizeof(T);
+    off = (tid / L::NC) * ldb + min(tid % L::NC, dh / L::VE - 1) * 16;
+  }
+  // rows row0 .. of g; rows past `last` read as row `last`
+  __device__ __forceinline__ void load(const T* __restrict__ g, int row0, int last, int tid) {
+    const char* p = reinterpret_cast<const char*>(g) + (long)row0 * ldb;
+    if (row0 + KB - 1 <= last) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-      const int i = tid + NT * k, r = i / L::NC, ch = i % L::NC;
-      v[k] = u32x4{0, 0, 0, 0};
-      if (ch * L::VE < dh)
-        v[k] = *reinterpret_cast<const u32x4*>(g + (long)min(row0 + r, last) * ld + ch * L::VE);
+      for (int k = 0; k < N; ++k)
+        v[k] = *reinterpret_cast<const u32x4*>(p + (long)k * STEP * ldb + off);
+    } else {
+      const unsigned r = tid / L::NC, c = off - r * ldb;
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+        v[k] = *reinterpret_cast<const u32x4*>(p + min(r + k * STEP, (unsigned)(last - row0)) * ldb + c);
     }
   }
   __device__ __forceinline__ void store(T* lds, int tid) const {
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      const int i = tid + NT * k;
-      *reinterpret_cast<u32x4*>(lds + L::at(i / L::NC, i % L::NC)) = v[k];
+      // (the swizzle repeats every 16 rows)
+      const int a = STEP % 16 ? L::at(tid / L::NC + k * STEP, tid % L::NC)
+                              : L::at(tid / L::NC, tid % L::NC) + k * STEP * DH;
+      *reinterpret_cast<u32x4*>(lds + a) = v[k];
     }
   }
 };
@@ -128,17 +149,18 @@ __device__ __forceinline__ f32x8 gfrag(const float* p, int g, int c, int dh) {
   return z;
 }
 
-// The same of a row of an LDS tile.
+// The same of row row0 + row of an LDS tile (row0 a multiple of 16, which leaves the
+// swizzle alone).
 template <int DH, int NG>
-__device__ __forceinline__ bf16x8 frag(const bf16_t* lds, int row, int g, int c) {
-  return *reinterpret_cast<const bf16x8*>(lds + Tile<bf16_t, DH>::at(row, NG * c + g));
+__device__ __forceinline__ bf16x8 frag(const bf16_t* lds, int row0, int row, int g, int c) {
+  return *reinterpret_cast<const bf16x8*>(lds + Tile<bf16_t, DH>::at(row, NG * c + g) + row0 * DH);
 }
 template <int DH, int NG>
-__device__ __forceinline__ f32x8 frag(const float* lds, int row, int g, int c) {
+__device__ __forceinline__ f32x8 frag(const float* lds, int row0, int row, int g, int c) {
   typedef Tile<float, DH> L;
   f32x8 v;
-  const f32x4 a = *reinterpret_cast<const f32x4*>(lds + L::at(row, 2 * (NG * c + g)));
-  const f32x4 b = *reinterpret_cast<const f32x4*>(lds + L::at(row, 2 * (NG * c + g) + 1));
+  const f32x4 a = *reinterpret_cast<const f32x4*>(lds + L::at(row, 2 * (NG * c + g)) + row0 * DH);
+  const f32x4 b = *reinterpret_cast<const f32x4*>(lds + L::at(row, 2 * (NG * c + g) + 1) + row0 * DH);
 #pragma unroll
   for (int t = 0; t < 4; ++t) { v.v[t] = a[t]; v.v[4 + t] = b[t]; }
   return v;
@@ -154,10 +176,9 @@ template <int DH, int R>
 __device__ __forceinline__ bf16x8 tfrag(const bf16_t* lds, int e, int lane, int c) {
   constexpr int NG = 64 / R;
   const int g = lane / R, i = lane & 15, sub = (lane % R) >> 4;
-  const int row = 8 * NG * c + 4 * g + (i >> 2);
-  const int ch = (e * R + 16 * sub) / 8 + ((i >> 1) & 1);
-  const bf16_t* p = lds + Tile<bf16_t, DH>::at(row, ch) + (i & 1) * 4;
-  const bf16_t* q = lds + Tile<bf16_t, DH>::at(row + 4 * NG, ch) + (i & 1) * 4;
+  const int row = 4 * g + (i >> 2), ch = (e * R + 16 * sub) / 8 + ((i >> 1) & 1);
+  const bf16_t* p = lds + Tile<bf16_t, DH>::at(row, ch) + (i & 1) * 4 + 8 * NG * c * DH;
+  const bf16_t* q = lds + Tile<bf16_t, DH>::at(row + 4 * NG, ch) + (i & 1) * 4 + 8 * NG * c * DH;
   union {
     v4s h[2];
     bf16x8 v;
@@ -174,7 +195,7 @@ __device__ __forceinline__ f32x8 tfrag(const float* lds, int e, int lane, int c)
   f32x8 v;
 #pragma unroll
   for (int t = 0; t < 8; ++t)
-    v.v[t] = lds[L::at(8 * NG * c + 4 * NG * (t / 4) + 4 * g + t % 4, col / 4) + (col & 3)];
+    v.v[t] = lds[L::at(4 * NG * (t / 4) + 4 * g + t % 4, col / 4) + (col & 3) + 8 * NG * c * DH];
   return v;
 }
 
@@ -194,6 +215,7 @@ __device__ __forceinline__ void pack(const V* s, int c, f32x8& f) {
   for (int t = 0; t < 8; ++t) f.v[t] = s[(8 * c + t) / AV][(8 * c + t) % AV];
 }
 
+// Sum and maximum over the lane groups (the lanes of one row).
 template <int R>
 __device__ __forceinline__ float sum_groups(float v) {
   if (R == 16) v += __shfl_xor(v, 16, 64);
@@ -280,12 +302,18 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<
     if constexpr (DUAL) zero(od[e]);
   }
   Block<T, DH, KB, NT> rK, rV, rKd, rVd;
+  rK.init(a.ldk, dh, tid);
+  rV.init(a.ldv, dh, tid);
+  if constexpr (DUAL) {
+    rKd.init(a.ldkd, dh, tid);
+    rVd.init(a.ldvd, dh, tid);
+  }
   auto load = [&](int k0) {
-    rK.load(K, a.ldk, k0, hi - 1, dh, tid);
-    rV.load(Vp, a.ldv, k0, hi - 1, dh, tid);
+    rK.load(K, k0, hi - 1, tid);
+    rV.load(Vp, k0, hi - 1, tid);
     if constexpr (DUAL) {
-      rKd.load(Kd, a.ldkd, k0, hi - 1, dh, tid);
-      rVd.load(Vd, a.ldvd, k0, hi - 1, dh, tid);
+      rKd.load(Kd, k0, hi - 1, tid);
+      rVd.load(Vd, k0, hi - 1, tid);
     }
   };
   auto store = [&](int b) {
@@ -299,9 +327,10 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<
   const int nb = (min(tile.x + NW * R, hi) - 1 - lo) / KB + 1;
   load(lo);
   store(0);
-  for (int kb = 0; kb < nb; ++kb) {
+  auto block = [&](int kb, auto buffer) {
+    constexpr int b = decltype(buffer)::value;
     __syncthreads();   // block kb is in its buffer, and nobody reads the other one
-    const int k0 = lo + kb * KB, b = kb & 1;
+    const int k0 = lo + kb * KB;
     if (kb + 1 < nb) load(k0 + KB);
 #pragma unroll
     for (int sb = 0; sb < KB / SB; ++sb) {
@@ -314,11 +343,11 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<
         if constexpr (DUAL) zero(sd[n]);
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-          const F kf = frag<DH, NG>(sK[b], sb * SB + n * R + lr, g, c);
+          const F kf = frag<DH, NG>(sK[b], sb * SB + n * R, lr, g, c);
           s[n] = mma(kf, qf[c], s[n]);
           if constexpr (DUAL) {
             sd[n] = mma(kf, qdf[c], sd[n]);
-            sd[n] = mma(frag<DH, NG>(sKd[b], sb * SB + n * R + lr, g, c), qf[c], sd[n]);
+            sd[n] = mma(frag<DH, NG>(sKd[b], sb * SB + n * R, lr, g, c), qf[c], sd[n]);
           }
         }
       }
@@ -334,9 +363,8 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<
 #pragma unroll
       for (int t = 0; t < NS * AV; ++t) mx = fmaxf(mx, s[t / AV][t % AV]);
       // the first keys hold a visible one of every query: m is finite from then on
-      mx = max_groups<R>(mx) * s2;
-      if (__any(mx > m + 8.f)) {
-        const float mn = fmaxf(m, mx), al = exp2_(m - mn);
+      if (__any(mx * s2 > m + 8.f)) {
+        const float mn = fmaxf(m, max_groups<R>(mx) * s2), al = exp2_(m - mn);
         m = mn;
         l *= al;
         if constexpr (DUAL) cs *= al;
@@ -374,6 +402,10 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<
       }
     }
     if (kb + 1 < nb) store(b ^ 1);
+  };
+  for (int kb = 0; kb < nb; kb += 2) {   // (buffers at constant addresses)
+    block(kb, std::integral_constant<int, 0>());
+    if (kb + 1 < nb) block(kb + 1, std::integral_constant<int, 1>());
   }
   if (q >= hi) return;   // (lanes of one row leave together; q0 < hi has l > 0)
   const float lt = sum_groups<R>(l), inv = 1.0f / lt;
@@ -458,12 +490,18 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T
     if constexpr (DUAL) zero(dqd[e]);
   }
   Block<T, DH, KB, NT> rK, rV, rKd, rVd;
+  rK.init(a.ldk, dh, tid);
+  rV.init(a.ldv, dh, tid);
+  if constexpr (DUAL) {
+    rKd.init(a.ldkd, dh, tid);
+    rVd.init(a.ldvd, dh, tid);
+  }
   auto load = [&](int k0) {
-    rK.load(K, a.ldk, k0, hi - 1, dh, tid);
-    rV.load(Vp, a.ldv, k0, hi - 1, dh, tid);
+    rK.load(K, k0, hi - 1, tid);
+    rV.load(Vp, k0, hi - 1, tid);
     if constexpr (DUAL) {
-      rKd.load(Kd, a.ldkd, k0, hi - 1, dh, tid);
-      rVd.load(Vd, a.ldvd, k0, hi - 1, dh, tid);
+      rKd.load(Kd, k0, hi - 1, tid);
+      rVd.load(Vd, k0, hi - 1, tid);
     }
   };
   auto store = [&](int b) {
@@ -477,9 +515,10 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T
   const int nb = (min(tile.x + NW * R, hi) - 1 - lo) / KB + 1;
   load(lo);
   store(0);
-  for (int kb = 0; kb < nb; ++kb) {
+  auto block = [&](int kb, auto buffer) {
+    constexpr int b = decltype(buffer)::value;
     __syncthreads();
-    const int k0 = lo + kb * KB, b = kb & 1;
+    const int k0 = lo + kb * KB;
     if (kb + 1 < nb) load(k0 + KB);
 #pragma unroll
     for (int sb = 0; sb < KB / SB; ++sb) {
@@ -493,15 +532,15 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T
         zero(s); zero(sd); zero(dp); zero(dpd);
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-          const int kr = sb * SB + n * R + lr;
-          const F kf = frag<DH, NG>(sK[b], kr, g, c), vf = frag<DH, NG>(sV[b], kr, g, c);
+          const int kr = sb * SB + n * R;
+          const F kf = frag<DH, NG>(sK[b], kr, lr, g, c), vf = frag<DH, NG>(sV[b], kr, lr, g, c);
           s = mma(kf, qf[c], s);
           dp = mma(vf, gf[c], dp);
           if constexpr (DUAL) {
             sd = mma(kf, qdf[c], sd);
-            sd = mma(frag<DH, NG>(sKd[b], kr, g, c), qf[c], sd);
+            sd = mma(frag<DH, NG>(sKd[b], kr, lr, g, c), qf[c], sd);
             dpd = mma(vf, gdf[c], dpd);
-            dpd = mma(frag<DH, NG>(sVd[b], kr, g, c), gf[c], dpd);
+            dpd = mma(frag<DH, NG>(sVd[b], kr, lr, g, c), gf[c], dpd);
           }
         }
 #pragma unroll
@@ -540,6 +579,10 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T
       }
     }
     if (kb + 1 < nb) store(b ^ 1);
+  };
+  for (int kb = 0; kb < nb; kb += 2) {   // (buffers at constant addresses)
+    block(kb, std::integral_constant<int, 0>());
+    if (kb + 1 < nb) block(kb + 1, std::integral_constant<int, 1>());
   }
   if (q >= hi) return;
   store_row<R, NE>(a.dq + q * a.lddq + (long)h * dh, dq, a.scale, g, dh);
@@ -592,15 +635,21 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dkv_kernel(PackedAttnArgs<
     }
   }
   Block<T, DH, KB, NT> rQ, rG, rQd, rGd;
+  rQ.init(a.ldq, dh, tid);
+  rG.init(a.ldg, dh, tid);
+  if constexpr (DUAL) {
+    rQd.init(a.ldqd, dh, tid);
+    rGd.init(a.ldgd, dh, tid);
+  }
   float xL = 0.f, xR = 0.f, xC = 0.f, xRd = 0.f;   // a query's row values (threads 0 .. 63)
   const int nq = (hi - tile.x + KB - 1) / KB, nb = nq * GP;
   auto load = [&](int i) {   // block i: query head i / nq, its block i % nq
     const int hq = i / nq, h = h0 + hq, r0 = tile.x + (i - hq * nq) * KB;
-    rQ.load(a.q + (long)h * dh, a.ldq, r0, hi - 1, dh, tid);
-    rG.load(a.g + (long)h * dh, a.ldg, r0, hi - 1, dh, tid);
+    rQ.load(a.q + (long)h * dh, r0, hi - 1, tid);
+    rG.load(a.g + (long)h * dh, r0, hi - 1, tid);
     if constexpr (DUAL) {
-      rQd.load(a.qd + (long)h * dh, a.ldqd, r0, hi - 1, dh, tid);
-      rGd.load(a.gd + (long)h * dh, a.ldgd, r0, hi - 1, dh, tid);
+      rQd.load(a.qd + (long)h * dh, r0, hi - 1, tid);
+      rGd.load(a.gd + (long)h * dh, r0, hi - 1, tid);
     }
     const long x = (long)h * a.p.n + min(r0 + (tid & (KB - 1)), hi - 1);
     xL = a.lse[x];
@@ -629,9 +678,9 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dkv_kernel(PackedAttnArgs<
   load(0);
   store(0);
   int r0 = tile.x;   // first query of the block
-  for (int i = 0; i < nb; ++i) {
+  auto block = [&](int i, auto buffer) {
+    constexpr int b = decltype(buffer)::value;
     __syncthreads();
-    const int b = i & 1;
     if (i + 1 < nb) load(i + 1);
 #pragma unroll
     for (int sb = 0; sb < KB / SB; ++sb) {
@@ -645,15 +694,15 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dkv_kernel(PackedAttnArgs<
         zero(s); zero(sd); zero(dp); zero(dpd);
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-          const int qr = sb * SB + n * R + lr;
-          const F qq = frag<DH, NG>(sQ[b], qr, g, c), gg = frag<DH, NG>(sG[b], qr, g, c);
+          const int qr = sb * SB + n * R;
+          const F qq = frag<DH, NG>(sQ[b], qr, lr, g, c), gg = frag<DH, NG>(sG[b], qr, lr, g, c);
           s = mma(qq, kf[c], s);
           dp = mma(gg, vf[c], dp);
           if constexpr (DUAL) {
             sd = mma(qq, kdf[c], sd);
-            sd = mma(frag<DH, NG>(sQd[b], qr, g, c), kf[c], sd);
+            sd = mma(frag<DH, NG>(sQd[b], qr, lr, g, c), kf[c], sd);
             dpd = mma(gg, vdf[c], dpd);
-            dpd = mma(frag<DH, NG>(sGd[b], qr, g, c), vf[c], dpd);
+            dpd = mma(frag<DH, NG>(sGd[b], qr, lr, g, c), vf[c], dpd);
           }
         }
 #pragma unroll
@@ -713,6 +762,10 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dkv_kernel(PackedAttnArgs<
     r0 += KB;
     if (r0 >= hi) r0 = tile.x;
     if (i + 1 < nb) store(b ^ 1);
+  };
+  for (int i = 0; i < nb; i += 2) {
+    block(i, std::integral_constant<int, 0>());
+    if (i + 1 < nb) block(i + 1, std::integral_constant<int, 1>());
   }
   if (k >= hi) return;
   if (a.parts > 1) {
