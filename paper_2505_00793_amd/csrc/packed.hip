@@ -280,7 +280,8 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<
   if (rank >= a.p.head[tile_kind(NW * R)]) return;
   const int4 tile = tl.byq[rank];
   const int lo = tile.y, hi = tile.z;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, lr = lane % R, g = lane / R;
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane % R, g = lane / R;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int q0 = tile.x + w * R, q = q0 + lr, qc = min(q, hi - 1);
   const int kh = h / (a.H / a.K), dh = a.dh;
   const T* K = a.k + (long)kh * dh;
@@ -452,7 +453,8 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T
   if (rank >= a.p.head[tile_kind(NW * R)]) return;
   const int4 tile = tl.byq[rank];
   const int lo = tile.y, hi = tile.z;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, lr = lane % R, g = lane / R;
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane % R, g = lane / R;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int q0 = tile.x + w * R, q = q0 + lr, qc = min(q, hi - 1);
   const int kh = h / (a.H / a.K), dh = a.dh;
   const T* K = a.k + (long)kh * dh;
@@ -543,6 +545,11 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T
             dpd = mma(frag<DH, NG>(sVd[b], kr, lr, g, c), gf[c], dpd);
           }
         }
+        if (diag) {   // some key may follow some query: its weight is 2^-inf = 0
+#pragma unroll
+          for (int t = 0; t < AV; ++t)
+            if (ks + n * R + 4 * NG * (t / 4) + 4 * g + t % 4 > q) s[t] = -INFINITY;
+        }
 #pragma unroll
         for (int t = 0; t < AV; ++t) {
           const float p = exp2_(fmaf(s[t], s2, -lse));
@@ -552,14 +559,6 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T
             const float pd = p * fmaf(sd[t], a.scale, -cst);
             dsd[n][t] = fmaf(pd, x, p * (dpd[t] - rd));
           }
-        }
-        if (diag) {
-#pragma unroll
-          for (int t = 0; t < AV; ++t)
-            if (ks + n * R + 4 * NG * (t / 4) + 4 * g + t % 4 > q) {
-              ds[n][t] = 0.f;
-              if constexpr (DUAL) dsd[n][t] = 0.f;
-            }
         }
       }
 #pragma unroll
@@ -609,7 +608,8 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dkv_kernel(PackedAttnArgs<
   if (rank >= a.p.head[tile_kind(NW * R)]) return;
   const int4 tile = tl.byk[rank];
   const int kh = hp / a.parts, part = hp - kh * a.parts, hi = tile.z;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, lr = lane % R, g = lane / R;
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane % R, g = lane / R;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int k0 = tile.x + w * R, k = k0 + lr, kc = min(k, hi - 1);
   const int GP = a.H / a.K / a.parts, dh = a.dh;   // query heads of a part
   const int h0 = (kh * a.parts + part) * GP;
@@ -705,6 +705,13 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dkv_kernel(PackedAttnArgs<
             dpd = mma(frag<DH, NG>(sGd[b], qr, lr, g, c), vf[c], dpd);
           }
         }
+        if (mask) {   // (weight 0, as above)
+#pragma unroll
+          for (int t = 0; t < AV; ++t) {
+            const int i1 = qs + n * R + 4 * NG * (t / 4) + 4 * g + t % 4;
+            if (i1 < k || i1 >= hi) s[t] = -INFINITY;
+          }
+        }
 #pragma unroll
         for (int t4 = 0; t4 < AV; t4 += 4) {
           const int i4 = sb * SB + n * R + NG * t4 + 4 * g;   // four queries of the block
@@ -718,19 +725,13 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dkv_kernel(PackedAttnArgs<
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
             const int t = t4 + u;
-            float pv = exp2_(fmaf(s[t], s2, -Lq[u]));
-            float x = dp[t] - Rq[u], y = 0.f, z = 0.f;
-            if constexpr (DUAL) {
-              y = fmaf(sd[t], a.scale, -Cq[u]);
-              z = dpd[t] - Dq[u];
-            }
-            if (mask && !(r0 + i4 + u >= k && r0 + i4 + u < hi)) pv = x = y = z = 0.f;
+            const float pv = exp2_(fmaf(s[t], s2, -Lq[u])), x = dp[t] - Rq[u];
             p[n][t] = pv;
             ds[n][t] = pv * x;
             if constexpr (DUAL) {
-              const float pdv = pv * y;
+              const float pdv = pv * fmaf(sd[t], a.scale, -Cq[u]);
               pd[n][t] = pdv;
-              dsd[n][t] = fmaf(pdv, x, pv * z);
+              dsd[n][t] = fmaf(pdv, x, pv * (dpd[t] - Dq[u]));
             }
           }
         }
