@@ -150,9 +150,9 @@ def _batch(x, y):
     return mfmg_batch(x.data_ptr(), None if y is None else y.data_ptr(), x.shape[0])
 
 
-def _stream():
+def _stream(device=None):
     import torch
-    return c_void_p(torch.cuda.current_stream().cuda_stream)
+    return torch.cuda.current_stream(device).cuda_stream
 
 
 def make_desc(*, widths, act=0, loss=1, optimizer=0, meta=0, precision=0, has_bias=True, rows=1,
@@ -260,15 +260,24 @@ def _bad(message: str):
     return MfmgError(ERR_INVALID_ARGUMENT, f"MFMG_ERR_INVALID_ARGUMENT: {message}")
 
 
-def _check_dev(name, t, dtype):
-    """t is a tensor of dtype on the current device (None passes)."""
-    import torch
+def _check_dev(name, t, dtype, device: int):
+    """t is a tensor of dtype on the device (None passes)."""
     if t is None:
         return
     if t.dtype != dtype:
         raise _bad(f"{name}: {t.dtype}, expected {dtype}")
-    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+    if t.get_device() != device:
         raise _bad(f"{name} is on {t.device}, expected the current device")
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _device() -> int:
+    """The current CUDA device (0 where there is none: no tensor is on it)."""
+    import torch
+    return torch.cuda.current_device() if torch.cuda.is_initialized() else 0
 
 
 class SeqPlan:
@@ -282,8 +291,9 @@ def mfmg_seq_plan(cu_seqlens, n_tokens: int, positions=None, plan=None) -> SeqPl
     """Plan of n_tokens rows holding len(cu_seqlens) - 1 sequences; `plan` reuses the device
     memory of an earlier one of the same sizes."""
     import torch
-    _check_dev("cu_seqlens", cu_seqlens, torch.int32)
-    _check_dev("positions", positions, torch.int32)
+    device = _device()
+    _check_dev("cu_seqlens", cu_seqlens, torch.int32, device)
+    _check_dev("positions", positions, torch.int32, device)
     m = cu_seqlens.numel() - 1
     if m < 0 or not cu_seqlens.is_contiguous():
         raise _bad("cu_seqlens must be contiguous with at least one entry")
@@ -295,8 +305,8 @@ def mfmg_seq_plan(cu_seqlens, n_tokens: int, positions=None, plan=None) -> SeqPl
         plan = SeqPlan(torch.empty(n.value, dtype=torch.uint8, device=cu_seqlens.device), n_tokens, m)
     elif (plan.n_tokens, plan.n_seqs) != (n_tokens, m):
         raise _bad("the plan to reuse is of other sizes")
-    _check_dev("plan", plan.data, torch.uint8)
-    check(lib().mfmg_seq_plan(_ptr(cu_seqlens), m, n_tokens, _ptr(positions), _ptr(plan.data),
+    _check_dev("plan", plan.data, torch.uint8, device)
+    check(lib().mfmg_seq_plan(_addr(cu_seqlens), m, n_tokens, _addr(positions), _addr(plan.data),
                               plan.data.numel(), _stream()))
     return plan
 
@@ -311,8 +321,12 @@ class Attention:
         check(lib().mfmg_attn_create(ctypes.byref(desc), ctypes.byref(self._h)))
         self.desc = desc
         self.dtype = torch.bfloat16 if desc.precision == 1 else torch.float32
+        self.float32 = torch.float32
+        self.uint8 = torch.uint8
         self.q_cols = desc.heads * desc.head_dim
         self.kv_cols = desc.kv_heads * desc.head_dim
+        self.cols = self.q_cols + 2 * self.kv_cols
+        self.gain_shape = (2, desc.head_dim)
 
     def __del__(self):
         h = getattr(self, "_h", None)
@@ -331,99 +345,102 @@ class Attention:
         return torch.empty(max(self.mfmg_attn_ws_bytes(n_tokens), 1), dtype=torch.uint8, device=device)
 
     @staticmethod
-    def _rows(name, t, cols, dtype, n):
-        """The leading dimension of row tensor t (0: None)."""
-        if t is None:
-            return 0
-        _check_dev(name, t, dtype)
-        if t.dim() != 2 or t.shape[0] != n or t.shape[1] != cols:
+    def _rows(name, t, cols, dtype, n, device):
+        """The leading dimension of row tensor t."""
+        if t.dtype != dtype or t.get_device() != device:
+            _check_dev(name, t, dtype, device)
+        if t.shape != (n, cols):
             raise _bad(f"{name}: shape {tuple(t.shape)}, expected ({n}, {cols})")
-        if n and t.stride(1) != 1:
+        if n < 2:
+            return cols
+        ld, one = t.stride()
+        if one != 1:
             raise _bad(f"{name}: rows are not contiguous")
-        return t.stride(0) if n > 1 else cols
+        return ld
 
-    def _pair(self, name, t, td, cols, dtype, n):
-        """The one leading dimension of an array and its tangent."""
-        ld = self._rows(name, t, cols, dtype, n)
-        ldd = self._rows(name + "d", td, cols, dtype, n)
-        if td is not None and t is not None and ld != ldd:
-            raise _bad(f"{name} and {name}d have different row strides")
-        return ld if t is not None else ldd
+    def _pair(self, name, t, td, cols, dtype, n, device):
+        """The one leading dimension of an array and its tangent (either may be None)."""
+        ld = 0 if t is None else self._rows(name, t, cols, dtype, n, device)
+        if td is not None:
+            ldd = self._rows(name + "d", td, cols, dtype, n, device)
+            if t is not None and ld != ldd:
+                raise _bad(f"{name} and {name}d have different row strides")
+            ld = ldd
+        return ld
 
-    def _gains(self, *ts):
-        import torch
+    def _gains(self, device, *ts):
         for name, t in zip(("gain", "gaind", "dgain", "dgaind"), ts):
             if t is not None:
-                _check_dev(name, t, torch.float32)
-                if tuple(t.shape) != (2, self.desc.head_dim) or not t.is_contiguous():
-                    raise _bad(f"{name}: expected a contiguous (2, {self.desc.head_dim})")
+                _check_dev(name, t, self.float32, device)
+                if t.shape != self.gain_shape or not t.is_contiguous():
+                    raise _bad(f"{name}: expected a contiguous {self.gain_shape}")
 
-    def _qkv(self, name, q, k, v, n):
+    def _qkv(self, name, q, k, v, n, device):
         """mfmg_qkv of three row tensors; None if none is given."""
         if q is None and k is None and v is None:
             return None
         if q is None or k is None or v is None:
             raise _bad(f"{name}: q, k and v go together")
-        ld = [self._rows(f"{name}.{c}", t, w, self.dtype, n)
-              for c, t, w in (("q", q, self.q_cols), ("k", k, self.kv_cols), ("v", v, self.kv_cols))]
-        return ctypes.byref(mfmg_qkv(q.data_ptr(), k.data_ptr(), v.data_ptr(), *ld))
+        rows = self._rows
+        return ctypes.byref(mfmg_qkv(
+            q.data_ptr(), k.data_ptr(), v.data_ptr(),
+            rows(name + ".q", q, self.q_cols, self.dtype, n, device),
+            rows(name + ".k", k, self.kv_cols, self.dtype, n, device),
+            rows(name + ".v", v, self.kv_cols, self.dtype, n, device)))
 
-    def _plan(self, plan, ws=None):
-        import torch
-        _check_dev("plan", plan.data, torch.uint8)
-        if ws is not None:
-            _check_dev("ws", ws, torch.uint8)
-        return self._h, _ptr(plan.data), plan.n_tokens, plan.n_seqs
+    def _head(self, plan, device, ws=None):
+        """The first arguments of every call."""
+        _check_dev("plan", plan.data, self.uint8, device)
+        _check_dev("ws", ws, self.uint8, device)
+        return self._h, plan.data.data_ptr(), plan.n_tokens, plan.n_seqs
 
     def mfmg_qk_rope_fwd(self, plan, x, y, gain=None, xd=None, gaind=None, yd=None):
-        import torch
-        n, w = plan.n_tokens, self.q_cols + 2 * self.kv_cols
-        ldx = self._pair("x", x, xd, w, torch.float32, n)
-        ldy = self._pair("y", y, yd, w, self.dtype, n)
-        self._gains(gain, gaind)
-        check(lib().mfmg_qk_rope_fwd(*self._plan(plan), _ptr(x), _ptr(xd), ldx, _ptr(gain),
-                                     _ptr(gaind), _ptr(y), _ptr(yd), ldy, _stream()))
+        n, w, dev = plan.n_tokens, self.cols, _device()
+        ldx = self._pair("x", x, xd, w, self.float32, n, dev)
+        ldy = self._pair("y", y, yd, w, self.dtype, n, dev)
+        self._gains(dev, gain, gaind)
+        check(lib().mfmg_qk_rope_fwd(*self._head(plan, dev), _addr(x), _addr(xd), ldx, _addr(gain),
+                                     _addr(gaind), _addr(y), _addr(yd), ldy, _stream(dev)))
 
     def mfmg_qk_rope_bwd(self, plan, dy, dx, x=None, gain=None, dgain=None, dyd=None, dxd=None,
                          xd=None, gaind=None, dgaind=None, ws=None):
-        import torch
-        n, w = plan.n_tokens, self.q_cols + 2 * self.kv_cols
-        ldx = self._pair("x", x, xd, w, torch.float32, n)
-        lddy = self._pair("dy", dy, dyd, w, self.dtype, n)
-        lddx = self._pair("dx", dx, dxd, w, self.dtype, n)
-        self._gains(gain, gaind, dgain, dgaind)
+        n, w, dev = plan.n_tokens, self.cols, _device()
+        ldx = self._pair("x", x, xd, w, self.float32, n, dev)
+        lddy = self._pair("dy", dy, dyd, w, self.dtype, n, dev)
+        lddx = self._pair("dx", dx, dxd, w, self.dtype, n, dev)
+        self._gains(dev, gain, gaind, dgain, dgaind)
         if ws is None:
             ws = self.workspace(n, dy.device)
-        check(lib().mfmg_qk_rope_bwd(*self._plan(plan, ws), _ptr(x), _ptr(xd), ldx, _ptr(gain),
-                                     _ptr(gaind), _ptr(dy), _ptr(dyd), lddy, _ptr(dx), _ptr(dxd), lddx,
-                                     _ptr(dgain), _ptr(dgaind), _ptr(ws), ws.numel(), _stream()))
+        check(lib().mfmg_qk_rope_bwd(*self._head(plan, dev, ws), _addr(x), _addr(xd), ldx, _addr(gain),
+                                     _addr(gaind), _addr(dy), _addr(dyd), lddy, _addr(dx), _addr(dxd),
+                                     lddx, _addr(dgain), _addr(dgaind), _addr(ws), ws.numel(), _stream(dev)))
 
-    def _stats(self, stats, n):
-        import torch
-        _check_dev("stats", stats, torch.float32)
+    def _stats(self, stats, n, device):
+        _check_dev("stats", stats, self.float32, device)
         if stats.numel() != 2 * self.desc.heads * n or not stats.is_contiguous():
             raise _bad(f"stats: expected a contiguous (2, {self.desc.heads}, {n})")
-        return _ptr(stats)
+        return stats.data_ptr()
 
     def mfmg_attn_fwd(self, plan, q, k, v, o, stats, qd=None, kd=None, vd=None, od=None):
-        n = plan.n_tokens
-        ldo = self._pair("o", o, od, self.q_cols, self.dtype, n)
-        check(lib().mfmg_attn_fwd(*self._plan(plan), self._qkv("x", q, k, v, n),
-                                  self._qkv("xd", qd, kd, vd, n), _ptr(o), _ptr(od), ldo,
-                                  self._stats(stats, n), _stream()))
+        n, dev = plan.n_tokens, _device()
+        ldo = self._pair("o", o, od, self.q_cols, self.dtype, n, dev)
+        check(lib().mfmg_attn_fwd(*self._head(plan, dev), self._qkv("x", q, k, v, n, dev),
+                                  self._qkv("xd", qd, kd, vd, n, dev), _addr(o), _addr(od), ldo,
+                                  self._stats(stats, n, dev), _stream(dev)))
 
     def mfmg_attn_bwd(self, plan, q, k, v, o, stats, g, dq, dk, dv, qd=None, kd=None, vd=None,
                       od=None, dod=None, dqd=None, dkd=None, dvd=None, ws=None):
-        n = plan.n_tokens
-        ldo = self._pair("o", o, od, self.q_cols, self.dtype, n)
-        ldg = self._pair("g", g, dod, self.q_cols, self.dtype, n)
+        n, dev = plan.n_tokens, _device()
+        ldo = self._pair("o", o, od, self.q_cols, self.dtype, n, dev)
+        ldg = self._pair("g", g, dod, self.q_cols, self.dtype, n, dev)
         if ws is None:
             ws = self.workspace(n, o.device)
-        check(lib().mfmg_attn_bwd(*self._plan(plan, ws), self._qkv("x", q, k, v, n),
-                                  self._qkv("xd", qd, kd, vd, n), _ptr(o), _ptr(od), ldo,
-                                  self._stats(stats, n), _ptr(g), _ptr(dod), ldg,
-                                  self._qkv("dx", dq, dk, dv, n), self._qkv("dxd", dqd, dkd, dvd, n),
-                                  _ptr(ws), ws.numel(), _stream()))
+        check(lib().mfmg_attn_bwd(*self._head(plan, dev, ws), self._qkv("x", q, k, v, n, dev),
+                                  self._qkv("xd", qd, kd, vd, n, dev), _addr(o), _addr(od), ldo,
+                                  self._stats(stats, n, dev), _addr(g), _addr(dod), ldg,
+                                  self._qkv("dx", dq, dk, dv, n, dev),
+                                  self._qkv("dxd", dqd, dkd, dvd, n, dev), _addr(ws), ws.numel(),
+                                  _stream(dev)))
 
 
 def mfmg_check_finite(x, ws=None) -> int:
