@@ -6,9 +6,11 @@
 
 namespace mfmg {
 
-// Attention tiles of two sizes: 64 and 128 rows (queries or keys).
-__host__ __device__ constexpr int tile_rows(int kind) { return kind ? 128 : 64; }
-__host__ __device__ constexpr int tile_kind(int rows) { return rows == 128 ? 1 : 0; }
+// Attention tiles of three sizes: 32, 64 and 128 rows (queries or keys).
+constexpr int TILE_KINDS = 3;
+__host__ __device__ constexpr int tile_rows(int kind) { return 32 << kind; }
+__host__ __device__ constexpr int tile_kind(int rows) { return rows == 128 ? 2 : rows == 64 ? 1 : 0; }
+constexpr int PLAN_FIRST = TILE_KINDS, PLAN_LAST = TILE_KINDS + 1;   // of SeqPlan::head
 constexpr int PK_MAX_DH = 128;      // largest head dimension
 constexpr long PK_MAX_TOKENS = (1L << 31) - 1024;
 constexpr int PK_MAX_SEQS = 1 << 24;
@@ -24,12 +26,12 @@ struct TileList {
   int4* byk;      // [max_tiles] as key tiles, by the queries that see them
 };
 struct SeqPlan {
-  int* head;      // [4] tiles of 64 rows, of 128 rows, b[0], b[m]
+  int* head;      // [TILE_KINDS + 2] tiles of each size, then b[0], b[m]
   int* bound;     // [m + 1] b
   int* pos;       // [n] rotary position of each token
-  TileList list[2];
+  TileList list[TILE_KINDS];
   long n;
-  int m, max_tiles[2];
+  int m, max_tiles[TILE_KINDS];
 };
 // Layout of a plan over n tokens and m sequences at `base` (null: measure);
 // *bytes receives its size.

@@ -37,19 +37,16 @@ namespace mfmg {
 
 namespace {
 
-constexpr int SB = 32;   // rows of a staged block that a wave forms and consumes scores of at a time
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 template <int R> struct AccT;
 template <> struct AccT<16> { typedef f32x4 V; };
 template <> struct AccT<32> { typedef f32x16 V; };
 
-struct f32x8 {
-  float v[8];
-};
+// Operand fragments: FE elements of a row.
 template <typename T> struct FragT;
-template <> struct FragT<bf16_t> { typedef bf16x8 V; };
-template <> struct FragT<float> { typedef f32x8 V; };
+template <> struct FragT<bf16_t> { typedef bf16x8 V; static constexpr int FE = 8; };
+template <> struct FragT<float> { typedef f32x4 V; static constexpr int FE = 4; };
 
 __device__ __forceinline__ f32x4 mma(const bf16x8& a, const bf16x8& b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
@@ -57,15 +54,10 @@ __device__ __forceinline__ f32x4 mma(const bf16x8& a, const bf16x8& b, f32x4 c) 
 __device__ __forceinline__ f32x16 mma(const bf16x8& a, const bf16x8& b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
-// float32: element t of every lane group's eight is one instruction's contraction
-__device__ __forceinline__ f32x4 mma(const f32x8& a, const f32x8& b, f32x4 c) {
+// float32: element t of every lane group's four is one instruction's contraction
+__device__ __forceinline__ f32x4 mma(const f32x4& a, const f32x4& b, f32x4 c) {
 #pragma unroll
-  for (int t = 0; t < 8; ++t) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[t], b.v[t], c, 0, 0, 0);
-  return c;
-}
-__device__ __forceinline__ f32x16 mma(const f32x8& a, const f32x8& b, f32x16 c) {
-#pragma unroll
-  for (int t = 0; t < 8; ++t) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[t], b.v[t], c, 0, 0, 0);
+  for (int t = 0; t < 4; ++t) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[t], b[t], c, 0, 0, 0);
   return c;
 }
 
@@ -78,11 +70,12 @@ __device__ __forceinline__ f32x16 mma(const f32x8& a, const f32x8& b, f32x16 c) 
 // 64-dim tiles were conflicts.)
 template <typename T, int DH>
 struct Tile {
-  static constexpr int VE = Elem<T>::VE, NC = DH / VE;   // chunks of a row
+  static constexpr int P = DH <= 64 ? 64 : 128;          // row pitch
+  static constexpr int VE = Elem<T>::VE, NC = P / VE;    // chunks of a row
   __device__ static __forceinline__ int at(int row, int chunk) {
     const int x = (row >> 2) & 3, h = ((x ^ (x >> 1)) & 1) << 1 | x >> 1;   // 0, 2, 3, 1
     const int f = sizeof(T) == 4 ? row & 15 : NC >= 16 ? (row & 3) << 2 | h : ((row >> 1) & 1) << 2 | h;
-    return row * DH + ((chunk ^ f) * VE);
+    return row * P + ((chunk ^ f) * VE);
   }
 };
 
@@ -124,16 +117,16 @@ struct Block {
     for (int k = 0; k < N; ++k) {
       // (the swizzle repeats every 16 rows)
       const int a = STEP % 16 ? L::at(tid / L::NC + k * STEP, tid % L::NC)
-                              : L::at(tid / L::NC, tid % L::NC) + k * STEP * DH;
+                              : L::at(tid / L::NC, tid % L::NC) + k * STEP * L::P;
       *reinterpret_cast<u32x4*>(lds + a) = v[k];
     }
   }
 };
 
-// Fragment c of a row in global memory: elements 8 NG c + 8 g .. + 7, zero past dh.
+// Fragment c of a row in global memory: elements FE (NG c + g) .. + FE - 1, zero past dh.
 template <int NG>
 __device__ __forceinline__ bf16x8 gfrag(const bf16_t* p, int g, int c, int dh) {
-  const int d = 8 * NG * c + 8 * g;
+  const int d = 8 * (NG * c + g);
   if (d < dh) return *reinterpret_cast<const bf16x8*>(p + d);
   bf16x8 z;
 #pragma unroll
@@ -141,32 +134,20 @@ __device__ __forceinline__ bf16x8 gfrag(const bf16_t* p, int g, int c, int dh) {
   return z;
 }
 template <int NG>
-__device__ __forceinline__ f32x8 gfrag(const float* p, int g, int c, int dh) {
-  const int d = 8 * NG * c + 8 * g;
-  f32x8 z;
-#pragma unroll
-  for (int t = 0; t < 8; ++t) z.v[t] = d < dh ? p[d + t] : 0.f;
-  return z;
+__device__ __forceinline__ f32x4 gfrag(const float* p, int g, int c, int dh) {
+  const int d = 4 * (NG * c + g);
+  return d < dh ? *reinterpret_cast<const f32x4*>(p + d) : f32x4{0.f, 0.f, 0.f, 0.f};
 }
 
 // The same of row row0 + row of an LDS tile (row0 a multiple of 16, which leaves the
 // swizzle alone).
-template <int DH, int NG>
-__device__ __forceinline__ bf16x8 frag(const bf16_t* lds, int row0, int row, int g, int c) {
-  return *reinterpret_cast<const bf16x8*>(lds + Tile<bf16_t, DH>::at(row, NG * c + g) + row0 * DH);
-}
-template <int DH, int NG>
-__device__ __forceinline__ f32x8 frag(const float* lds, int row0, int row, int g, int c) {
-  typedef Tile<float, DH> L;
-  f32x8 v;
-  const f32x4 a = *reinterpret_cast<const f32x4*>(lds + L::at(row, 2 * (NG * c + g)) + row0 * DH);
-  const f32x4 b = *reinterpret_cast<const f32x4*>(lds + L::at(row, 2 * (NG * c + g) + 1) + row0 * DH);
-#pragma unroll
-  for (int t = 0; t < 4; ++t) { v.v[t] = a[t]; v.v[4 + t] = b[t]; }
-  return v;
+template <typename T, int DH, int NG>
+__device__ __forceinline__ typename FragT<T>::V frag(const T* lds, int row0, int row, int g, int c) {
+  typedef Tile<T, DH> L;
+  return *reinterpret_cast<const typename FragT<T>::V*>(lds + L::at(row, NG * c + g) + row0 * L::P);
 }
 
-// Fragment c of column R e + (lane % R) of an LDS tile: rows 8 NG c + idx(t), t = 0..7.
+// Fragment c of column R e + (lane % R) of an LDS tile: rows idx(FE c + t), t < FE.
 // ds_read_b64_tr_b16 works on groups of 16 lanes: lane i reads 4 elements at its own
 // address and lane j gets element j % 4 of lanes j / 4, j / 4 + 4, + 8, + 12, so with
 // lane i at row i / 4 and columns 4 (i % 4) .. + 3, lane j holds 4 rows of column j.
@@ -175,10 +156,11 @@ typedef __attribute__((address_space(3))) v4s lds_v4s;
 template <int DH, int R>
 __device__ __forceinline__ bf16x8 tfrag(const bf16_t* lds, int e, int lane, int c) {
   constexpr int NG = 64 / R;
+  typedef Tile<bf16_t, DH> L;
   const int g = lane / R, i = lane & 15, sub = (lane % R) >> 4;
   const int row = 4 * g + (i >> 2), ch = (e * R + 16 * sub) / 8 + ((i >> 1) & 1);
-  const bf16_t* p = lds + Tile<bf16_t, DH>::at(row, ch) + (i & 1) * 4 + 8 * NG * c * DH;
-  const bf16_t* q = lds + Tile<bf16_t, DH>::at(row + 4 * NG, ch) + (i & 1) * 4 + 8 * NG * c * DH;
+  const bf16_t* p = lds + L::at(row, ch) + (i & 1) * 4 + 8 * NG * c * L::P;
+  const bf16_t* q = lds + L::at(row + 4 * NG, ch) + (i & 1) * 4 + 8 * NG * c * L::P;
   union {
     v4s h[2];
     bf16x8 v;
@@ -188,20 +170,19 @@ __device__ __forceinline__ bf16x8 tfrag(const bf16_t* lds, int e, int lane, int 
   return x.v;
 }
 template <int DH, int R>
-__device__ __forceinline__ f32x8 tfrag(const float* lds, int e, int lane, int c) {
+__device__ __forceinline__ f32x4 tfrag(const float* lds, int e, int lane, int c) {
   constexpr int NG = 64 / R;
   typedef Tile<float, DH> L;
   const int g = lane / R, col = e * R + lane % R;
-  f32x8 v;
+  f32x4 v;
 #pragma unroll
-  for (int t = 0; t < 8; ++t)
-    v.v[t] = lds[L::at(4 * NG * (t / 4) + 4 * g + t % 4, col / 4) + (col & 3) + 8 * NG * c * DH];
+  for (int t = 0; t < 4; ++t) v[t] = lds[L::at(4 * g + t, col / 4) + (col & 3) + 4 * NG * c * L::P];
   return v;
 }
 
-// Fragment c from the lane's own values (flat index 8 c .. 8 c + 7).  bf16 rounds P and
-// the score cotangents to nearest even: the products take bf16 operands, and the sums
-// of the softmax are taken from the float32 values before that.
+// Fragment c from the lane's own values (flat index FE c .. + FE - 1).  bf16 rounds P and
+// the score cotangents to nearest even: the products take bf16 operands, and the softmax
+// sums are taken from the float32 values before that.
 template <typename V>
 __device__ __forceinline__ void pack(const V* s, int c, bf16x8& f) {
   constexpr int AV = sizeof(V) / 4;
@@ -209,10 +190,10 @@ __device__ __forceinline__ void pack(const V* s, int c, bf16x8& f) {
   for (int t = 0; t < 8; ++t) f[t] = (__bf16)s[(8 * c + t) / AV][(8 * c + t) % AV];
 }
 template <typename V>
-__device__ __forceinline__ void pack(const V* s, int c, f32x8& f) {
+__device__ __forceinline__ void pack(const V* s, int c, f32x4& f) {
   constexpr int AV = sizeof(V) / 4;
 #pragma unroll
-  for (int t = 0; t < 8; ++t) f.v[t] = s[(8 * c + t) / AV][(8 * c + t) % AV];
+  for (int t = 0; t < 4; ++t) f[t] = s[(4 * c + t) / AV][(4 * c + t) % AV];
 }
 
 // Sum and maximum over the lane groups (the lanes of one row).
@@ -246,6 +227,32 @@ __device__ __forceinline__ void store_row(T* row, const V (&acc)[NE], float f, i
   }
 }
 
+// Two waves that own the same rows and every other SB of the other side (KS = 2) join
+// their sums in LDS, lane by lane: the odd wave's times f1 are added to the even wave's
+// times f0.  All waves call this together; `lds` is free for it.
+template <int R, int NE, int KS>
+struct Merge {
+  static constexpr int AV = R * R / 64, LANE = NE * AV + 3;   // floats of a lane: an array, 3 scalars
+  float* p;
+  bool odd;
+  __device__ __forceinline__ Merge(float* lds, int w, int lane)
+      : p(lds + w / KS * LANE * 64 + lane), odd(w % KS) {}
+  __device__ __forceinline__ float& scalar(int i) { return p[(NE * AV + i) * 64]; }
+  template <typename V>
+  __device__ __forceinline__ void add(V (&v)[NE], float f0, float f1) {
+    __syncthreads();
+    if (odd) {
+#pragma unroll
+      for (int t = 0; t < NE * AV; ++t) p[t * 64] = v[t / AV][t % AV];
+    }
+    __syncthreads();
+    if (!odd) {
+#pragma unroll
+      for (int t = 0; t < NE * AV; ++t) v[t / AV][t % AV] = v[t / AV][t % AV] * f0 + p[t * 64] * f1;
+    }
+  }
+};
+
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Rank (0 = most work) and head of this workgroup: ranks vary slowest, so the longest
@@ -265,24 +272,24 @@ __device__ __forceinline__ void tile_of(int heads, int& rank, int& head) {
 // more than 2^8: until then exp2 stays below 2^8 times its usual range, far from
 // float32's, and a factor common to numerator and denominator changes neither's
 // relative error.
-template <typename T, int DH, int R, int NW, int KB, int MW, bool DUAL>
+template <typename T, int DH, int R, int NW, int KS, int KB, int SB, int MW, bool DUAL>
 __global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<T> a) {
-  constexpr int NT = 64 * NW, NG = 64 / R, NS = SB / R, NE = DH / R, NC = DH / (8 * NG);
-  constexpr int AV = R * R / 64, NK = SB / (8 * NG);
+  constexpr int NT = 64 * NW, NG = 64 / R, NS = SB / R, NE = DH / R, FE = FragT<T>::FE, NC = DH / (FE * NG);
+  constexpr int AV = R * R / 64, NK = SB / (FE * NG), ROWS = NW * R / KS;
   typedef typename AccT<R>::V V;
   typedef typename FragT<T>::V F;
   typedef Tile<T, DH> L;
-  __shared__ __attribute__((aligned(16))) T sK[2][KB * DH], sV[2][KB * DH],
-      sKd[DUAL ? 2 : 1][DUAL ? KB * DH : 8], sVd[DUAL ? 2 : 1][DUAL ? KB * DH : 8];
+  __shared__ __attribute__((aligned(16))) T sK[2][KB * L::P], sV[2][KB * L::P],
+      sKd[DUAL ? 2 : 1][DUAL ? KB * L::P : 8], sVd[DUAL ? 2 : 1][DUAL ? KB * L::P : 8];
   int rank, h;
   tile_of(a.H, rank, h);
-  const TileList tl = a.p.list[tile_kind(NW * R)];
-  if (rank >= a.p.head[tile_kind(NW * R)]) return;
-  const int4 tile = tl.byq[rank];
+  const TileList tl = a.p.list[tile_kind(ROWS)];
+  const int4 tile = tl.byq[rank];   // (its load does not wait for the count)
+  if (rank >= a.p.head[tile_kind(ROWS)]) return;
   const int lo = tile.y, hi = tile.z;
   const int tid = threadIdx.x, lane = tid & 63, lr = lane % R, g = lane / R;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int q0 = tile.x + w * R, q = q0 + lr, qc = min(q, hi - 1);
+  const int q0 = tile.x + w / KS * R, q = q0 + lr, qc = min(q, hi - 1);
   const int kh = h / (a.H / a.K), dh = a.dh;
   const T* K = a.k + (long)kh * dh;
   const T* Vp = a.v + (long)kh * dh;
@@ -325,7 +332,7 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<
       rVd.store(sVd[b], tid);
     }
   };
-  const int nb = (min(tile.x + NW * R, hi) - 1 - lo) / KB + 1;
+  const int nb = (min(tile.x + ROWS, hi) - 1 - lo) / KB + 1;
   load(lo);
   store(0);
   auto block = [&](int kb, auto buffer) {
@@ -336,6 +343,7 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<
 #pragma unroll
     for (int sb = 0; sb < KB / SB; ++sb) {
       const int ks = k0 + sb * SB;
+      if (KS > 1 && sb % KS != w % KS) continue;
       if (ks > q0 + R - 1 || q0 >= hi) break;   // nothing further is visible to the wave
       V s[NS], sd[DUAL ? NS : 1];
 #pragma unroll
@@ -344,11 +352,11 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<
         if constexpr (DUAL) zero(sd[n]);
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-          const F kf = frag<DH, NG>(sK[b], sb * SB + n * R, lr, g, c);
+          const F kf = frag<T, DH, NG>(sK[b], sb * SB + n * R, lr, g, c);
           s[n] = mma(kf, qf[c], s[n]);
           if constexpr (DUAL) {
             sd[n] = mma(kf, qdf[c], sd[n]);
-            sd[n] = mma(frag<DH, NG>(sKd[b], sb * SB + n * R, lr, g, c), qf[c], sd[n]);
+            sd[n] = mma(frag<T, DH, NG>(sKd[b], sb * SB + n * R, lr, g, c), qf[c], sd[n]);
           }
         }
       }
@@ -408,6 +416,30 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<
     block(kb, std::integral_constant<int, 0>());
     if (kb + 1 < nb) block(kb + 1, std::integral_constant<int, 1>());
   }
+  if constexpr (KS > 1) {
+    // the other half of the keys joins in, both at the larger maximum
+    Merge<R, NE, KS> M(reinterpret_cast<float*>(&sK[0][0]), w, lane);
+    static_assert(NW / KS * M.LANE * 256 <= sizeof(sK), "merge buffer");
+    __syncthreads();
+    if (M.odd) {
+      M.scalar(0) = m;
+      M.scalar(1) = l;
+      M.scalar(2) = cs;
+    }
+    __syncthreads();
+    float f0 = 1.f, f1 = 1.f;
+    if (!M.odd) {   // (the even wave has seen the first key: its maximum is finite)
+      const float m1 = M.scalar(0), mn = fmaxf(m, m1);
+      f0 = exp2_(m - mn);
+      f1 = exp2_(m1 - mn);
+      m = mn;
+      l = l * f0 + M.scalar(1) * f1;
+      cs = cs * f0 + M.scalar(2) * f1;
+    }
+    M.add(o, f0, f1);
+    if constexpr (DUAL) M.add(od, f0, f1);
+    if (M.odd) return;
+  }
   if (q >= hi) return;   // (lanes of one row leave together; q0 < hi has l > 0)
   const float lt = sum_groups<R>(l), inv = 1.0f / lt;
   const float c = DUAL ? sum_groups<R>(cs) * inv : 0.f;
@@ -430,32 +462,29 @@ __device__ __forceinline__ float dot(const bf16x8& a, const bf16x8& b) {
   for (int t = 0; t < 8; ++t) s += (float)a[t] * (float)b[t];
   return s;
 }
-__device__ __forceinline__ float dot(const f32x8& a, const f32x8& b) {
-  float s = 0.f;
-#pragma unroll
-  for (int t = 0; t < 8; ++t) s += a.v[t] * b.v[t];
-  return s;
+__device__ __forceinline__ float dot(const f32x4& a, const f32x4& b) {
+  return a[0] * b[0] + a[1] * b[1] + a[2] * b[2] + a[3] * b[3];
 }
 
 // Scores' cotangents are formed without the scale s, which the sums take at the end.
-template <typename T, int DH, int R, int NW, int KB, int MW, bool DUAL>
+template <typename T, int DH, int R, int NW, int KS, int KB, int SB, int MW, bool DUAL>
 __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T> a) {
-  constexpr int NT = 64 * NW, NG = 64 / R, NS = SB / R, NE = DH / R, NC = DH / (8 * NG);
-  constexpr int AV = R * R / 64, NK = SB / (8 * NG);
+  constexpr int NT = 64 * NW, NG = 64 / R, NS = SB / R, NE = DH / R, FE = FragT<T>::FE, NC = DH / (FE * NG);
+  constexpr int AV = R * R / 64, NK = SB / (FE * NG), ROWS = NW * R / KS;
   typedef typename AccT<R>::V V;
   typedef typename FragT<T>::V F;
   typedef Tile<T, DH> L;
-  __shared__ __attribute__((aligned(16))) T sK[2][KB * DH], sV[2][KB * DH],
-      sKd[DUAL ? 2 : 1][DUAL ? KB * DH : 8], sVd[DUAL ? 2 : 1][DUAL ? KB * DH : 8];
+  __shared__ __attribute__((aligned(16))) T sK[2][KB * L::P], sV[2][KB * L::P],
+      sKd[DUAL ? 2 : 1][DUAL ? KB * L::P : 8], sVd[DUAL ? 2 : 1][DUAL ? KB * L::P : 8];
   int rank, h;
   tile_of(a.H, rank, h);
-  const TileList tl = a.p.list[tile_kind(NW * R)];
-  if (rank >= a.p.head[tile_kind(NW * R)]) return;
-  const int4 tile = tl.byq[rank];
+  const TileList tl = a.p.list[tile_kind(ROWS)];
+  const int4 tile = tl.byq[rank];   // (its load does not wait for the count)
+  if (rank >= a.p.head[tile_kind(ROWS)]) return;
   const int lo = tile.y, hi = tile.z;
   const int tid = threadIdx.x, lane = tid & 63, lr = lane % R, g = lane / R;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int q0 = tile.x + w * R, q = q0 + lr, qc = min(q, hi - 1);
+  const int q0 = tile.x + w / KS * R, q = q0 + lr, qc = min(q, hi - 1);
   const int kh = h / (a.H / a.K), dh = a.dh;
   const T* K = a.k + (long)kh * dh;
   const T* Vp = a.v + (long)kh * dh;
@@ -514,7 +543,7 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T
       rVd.store(sVd[b], tid);
     }
   };
-  const int nb = (min(tile.x + NW * R, hi) - 1 - lo) / KB + 1;
+  const int nb = (min(tile.x + ROWS, hi) - 1 - lo) / KB + 1;
   load(lo);
   store(0);
   auto block = [&](int kb, auto buffer) {
@@ -525,6 +554,7 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T
 #pragma unroll
     for (int sb = 0; sb < KB / SB; ++sb) {
       const int ks = k0 + sb * SB;
+      if (KS > 1 && sb % KS != w % KS) continue;
       if (ks > q0 + R - 1 || q0 >= hi) break;
       const bool diag = ks + SB - 1 > q0;
       V ds[NS], dsd[DUAL ? NS : 1];
@@ -535,14 +565,14 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
           const int kr = sb * SB + n * R;
-          const F kf = frag<DH, NG>(sK[b], kr, lr, g, c), vf = frag<DH, NG>(sV[b], kr, lr, g, c);
+          const F kf = frag<T, DH, NG>(sK[b], kr, lr, g, c), vf = frag<T, DH, NG>(sV[b], kr, lr, g, c);
           s = mma(kf, qf[c], s);
           dp = mma(vf, gf[c], dp);
           if constexpr (DUAL) {
             sd = mma(kf, qdf[c], sd);
-            sd = mma(frag<DH, NG>(sKd[b], kr, lr, g, c), qf[c], sd);
+            sd = mma(frag<T, DH, NG>(sKd[b], kr, lr, g, c), qf[c], sd);
             dpd = mma(vf, gdf[c], dpd);
-            dpd = mma(frag<DH, NG>(sVd[b], kr, lr, g, c), gf[c], dpd);
+            dpd = mma(frag<T, DH, NG>(sVd[b], kr, lr, g, c), gf[c], dpd);
           }
         }
         if (diag) {   // some key may follow some query: its weight is 2^-inf = 0
@@ -583,6 +613,13 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T
     block(kb, std::integral_constant<int, 0>());
     if (kb + 1 < nb) block(kb + 1, std::integral_constant<int, 1>());
   }
+  if constexpr (KS > 1) {
+    Merge<R, NE, KS> M(reinterpret_cast<float*>(&sK[0][0]), w, lane);
+    static_assert(NW / KS * M.LANE * 256 <= sizeof(sK), "merge buffer");
+    M.add(dq, 1.f, 1.f);
+    if constexpr (DUAL) M.add(dqd, 1.f, 1.f);
+    if (M.odd) return;
+  }
   if (q >= hi) return;
   store_row<R, NE>(a.dq + q * a.lddq + (long)h * dh, dq, a.scale, g, dh);
   if constexpr (DUAL) store_row<R, NE>(a.dqd + q * a.lddqd + (long)h * dh, dqd, a.scale, g, dh);
@@ -592,25 +629,25 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T
 // A workgroup owns NW R keys of one key head and goes through the queries of some of the
 // head's query heads (all, or one part of `parts`, whose float32 sums dkv_sum_kernel
 // adds in order).
-template <typename T, int DH, int R, int NW, int KB, int MW, bool DUAL>
+template <typename T, int DH, int R, int NW, int KS, int KB, int SB, int MW, bool DUAL>
 __global__ void __launch_bounds__(64 * NW, MW) packed_dkv_kernel(PackedAttnArgs<T> a) {
-  constexpr int NT = 64 * NW, NG = 64 / R, NS = SB / R, NE = DH / R, NC = DH / (8 * NG);
-  constexpr int AV = R * R / 64, NK = SB / (8 * NG);
+  constexpr int NT = 64 * NW, NG = 64 / R, NS = SB / R, NE = DH / R, FE = FragT<T>::FE, NC = DH / (FE * NG);
+  constexpr int AV = R * R / 64, NK = SB / (FE * NG), ROWS = NW * R / KS;
   typedef typename AccT<R>::V V;
   typedef typename FragT<T>::V F;
   typedef Tile<T, DH> L;
-  __shared__ __attribute__((aligned(16))) T sQ[2][KB * DH], sG[2][KB * DH],
-      sQd[DUAL ? 2 : 1][DUAL ? KB * DH : 8], sGd[DUAL ? 2 : 1][DUAL ? KB * DH : 8];
+  __shared__ __attribute__((aligned(16))) T sQ[2][KB * L::P], sG[2][KB * L::P],
+      sQd[DUAL ? 2 : 1][DUAL ? KB * L::P : 8], sGd[DUAL ? 2 : 1][DUAL ? KB * L::P : 8];
   __shared__ __attribute__((aligned(16))) float sL[2][KB], sR[2][KB], sC[2][KB], sRd[2][KB];
   int rank, hp;
   tile_of(a.K * a.parts, rank, hp);
-  const TileList tl = a.p.list[tile_kind(NW * R)];
-  if (rank >= a.p.head[tile_kind(NW * R)]) return;
+  const TileList tl = a.p.list[tile_kind(ROWS)];
   const int4 tile = tl.byk[rank];
+  if (rank >= a.p.head[tile_kind(ROWS)]) return;
   const int kh = hp / a.parts, part = hp - kh * a.parts, hi = tile.z;
   const int tid = threadIdx.x, lane = tid & 63, lr = lane % R, g = lane / R;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int k0 = tile.x + w * R, k = k0 + lr, kc = min(k, hi - 1);
+  const int k0 = tile.x + w / KS * R, k = k0 + lr, kc = min(k, hi - 1);
   const int GP = a.H / a.K / a.parts, dh = a.dh;   // query heads of a part
   const int h0 = (kh * a.parts + part) * GP;
   F kf[NC], vf[NC], kdf[DUAL ? NC : 1], vdf[DUAL ? NC : 1];
@@ -685,6 +722,7 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dkv_kernel(PackedAttnArgs<
 #pragma unroll
     for (int sb = 0; sb < KB / SB; ++sb) {
       const int qs = r0 + sb * SB;
+      if (KS > 1 && sb % KS != w % KS) continue;
       if (qs + SB - 1 < k0 || k0 >= hi || qs >= hi) continue;   // no query of these sees the wave's keys
       const bool mask = qs < k0 + R - 1 || qs + SB > hi;
       V p[NS], ds[NS], pd[DUAL ? NS : 1], dsd[DUAL ? NS : 1];
@@ -695,14 +733,14 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dkv_kernel(PackedAttnArgs<
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
           const int qr = sb * SB + n * R;
-          const F qq = frag<DH, NG>(sQ[b], qr, lr, g, c), gg = frag<DH, NG>(sG[b], qr, lr, g, c);
+          const F qq = frag<T, DH, NG>(sQ[b], qr, lr, g, c), gg = frag<T, DH, NG>(sG[b], qr, lr, g, c);
           s = mma(qq, kf[c], s);
           dp = mma(gg, vf[c], dp);
           if constexpr (DUAL) {
             sd = mma(qq, kdf[c], sd);
-            sd = mma(frag<DH, NG>(sQd[b], qr, lr, g, c), kf[c], sd);
+            sd = mma(frag<T, DH, NG>(sQd[b], qr, lr, g, c), kf[c], sd);
             dpd = mma(gg, vdf[c], dpd);
-            dpd = mma(frag<DH, NG>(sGd[b], qr, lr, g, c), vf[c], dpd);
+            dpd = mma(frag<T, DH, NG>(sGd[b], qr, lr, g, c), vf[c], dpd);
           }
         }
         if (mask) {   // (weight 0, as above)
@@ -768,6 +806,17 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dkv_kernel(PackedAttnArgs<
     block(i, std::integral_constant<int, 0>());
     if (i + 1 < nb) block(i + 1, std::integral_constant<int, 1>());
   }
+  if constexpr (KS > 1) {
+    Merge<R, NE, KS> M(reinterpret_cast<float*>(&sQ[0][0]), w, lane);
+    static_assert(NW / KS * M.LANE * 256 <= sizeof(sQ), "merge buffer");
+    M.add(dk, 1.f, 1.f);
+    M.add(dv, 1.f, 1.f);
+    if constexpr (DUAL) {
+      M.add(dkd, 1.f, 1.f);
+      M.add(dvd, 1.f, 1.f);
+    }
+    if (M.odd) return;
+  }
   if (k >= hi) return;
   if (a.parts > 1) {
     float* P = a.partial + (((long)part * a.p.n + k) * a.K + kh) * (DUAL ? 4 : 2) * dh;
@@ -794,7 +843,7 @@ __global__ void __launch_bounds__(256) dkv_sum_kernel(PackedAttnArgs<T> a) {
   const long i = (long)blockIdx.x * 256 + threadIdx.x;
   const int per = a.K * na * d4;   // fours of a token
   const long tok = i / per;
-  if (tok < a.p.head[2] || tok >= a.p.head[3]) return;
+  if (tok < a.p.head[PLAN_FIRST] || tok >= a.p.head[PLAN_LAST]) return;
   const int j = (int)(i - tok * per), d = 4 * (j % d4), k = j / d4 % na, kh = j / d4 / na;
   const float* P = a.partial + ((tok * a.K + kh) * na + k) * a.dh + d;
   f32x4 s = *reinterpret_cast<const f32x4*>(P);
@@ -806,8 +855,8 @@ __global__ void __launch_bounds__(256) dkv_sum_kernel(PackedAttnArgs<T> a) {
 }
 
 // ---------------------------------------------------------------- plan
-// Bounds made ascending (running maximum of the clamped offsets) and, for both tile
-// sizes, the tiles before each sequence, by one workgroup over chunks of its size.
+// Bounds made ascending (running maximum of the clamped offsets) and, for every tile
+// size, the tiles before each sequence, by one workgroup over chunks of its size.
 constexpr int SCAN = 1024;
 __global__ void __launch_bounds__(SCAN) plan_scan_kernel(SeqPlanArgs a) {
   __shared__ int sv[SCAN], carry;
@@ -833,7 +882,7 @@ __global__ void __launch_bounds__(SCAN) plan_scan_kernel(SeqPlanArgs a) {
     __syncthreads();
     if (tid == 0) carry = max(carry, sv[SCAN - 1]);
   }
-  for (int kind = 0; kind < 2; ++kind) {
+  for (int kind = 0; kind < TILE_KINDS; ++kind) {
     const int rows = tile_rows(kind);
     __syncthreads();
     if (tid == 0) carry = 0;
@@ -857,8 +906,8 @@ __global__ void __launch_bounds__(SCAN) plan_scan_kernel(SeqPlanArgs a) {
     if (tid == 0) a.p.head[kind] = carry;
   }
   if (tid == 0) {
-    a.p.head[2] = a.p.bound[0];
-    a.p.head[3] = a.p.bound[m];
+    a.p.head[PLAN_FIRST] = a.p.bound[0];
+    a.p.head[PLAN_LAST] = a.p.bound[m];
   }
 }
 
@@ -872,11 +921,11 @@ __device__ __forceinline__ int last_le(const int* x, int m, int v) {
   return lo;
 }
 
-// Workgroups 0 .. 3 write the tile lists (two sizes, by the keys a query tile sees and by
-// the queries that see a key tile), longest first, by counting into SCAN classes of
+// The first workgroups write the tile lists (of each size, by the keys a query tile sees and
+// by the queries that see a key tile), longest first, by counting into SCAN classes of
 // length; the order inside a class is free, since every tile's results are its own.
 // The others write the positions.
-constexpr int PLAN_LISTS = 4;
+constexpr int PLAN_LISTS = 2 * TILE_KINDS;
 __global__ void __launch_bounds__(SCAN) plan_fill_kernel(SeqPlanArgs a) {
   const int m = a.p.m, tid = threadIdx.x;
   if (blockIdx.x >= PLAN_LISTS) {
@@ -891,7 +940,7 @@ __global__ void __launch_bounds__(SCAN) plan_fill_kernel(SeqPlanArgs a) {
     return;
   }
   __shared__ int count[SCAN], longest;
-  const int kind = blockIdx.x & 1, byk = blockIdx.x >> 1, rows = tile_rows(kind);
+  const int kind = blockIdx.x >> 1, byk = blockIdx.x & 1, rows = tile_rows(kind);
   const TileList l = a.p.list[kind];
   const int nt = a.p.head[kind];
   count[tid] = 0;
@@ -936,39 +985,72 @@ int dkv_parts(long n, int H, int K) {
   return G;
 }
 
-// Rows a wave owns, waves of a workgroup, rows of a staged block, waves a SIMD holds.
+// Rows a wave owns, waves of a workgroup, waves that share rows, rows of a staged block, rows
+// of it that a wave forms and consumes scores of at a time, waves a SIMD holds.
 enum Pass { FWD, DQ, DKV };
-template <typename T, int DH, bool DUAL, int PASS>
+template <typename T, int DH, bool DUAL, int PASS, bool SMALL>
 struct Shape {
-  static constexpr bool F32 = sizeof(T) == 4, WIDE = !F32 && !DUAL && PASS != DKV;
-  static constexpr int R = WIDE ? 32 : 16;
-  static constexpr int NW = !F32 && DUAL && DH == 64 ? 8 : 4;
-  static constexpr int KB = (F32 && DH == 128 && DUAL) || (!F32 && DUAL && DH == 128 && PASS != DKV) ? 32 : 64;
-  static constexpr int MW = F32 || (DUAL && DH == 128 && PASS == DKV) ? 1 : 2;
+  static constexpr bool F32 = sizeof(T) == 4, BIG = DH > 64;
+  static constexpr int R = !F32 && !DUAL && PASS != DKV && !SMALL ? 32 : 16;
+  static constexpr int NW = !F32 && DUAL && !BIG && !SMALL ? 8 : 4;
+  static constexpr int KS = F32 && SMALL ? 2 : 1;
+  static constexpr int KB = BIG && DUAL && (F32 || PASS != DKV) ? 32 : 64;
+  static constexpr int SB = KB == 32 && KS == 2 ? 16 : 32;
+  static constexpr int MW = F32 || (DUAL && BIG && PASS == DKV) ? 1 : 2;
+  static constexpr int KIND = tile_kind(NW * R / KS);
 };
 
-template <typename T, int DH, bool DUAL>
+template <typename T, int DH, bool DUAL, bool SMALL>
 void launch_fwd(const PackedAttnArgs<T>& a, hipStream_t s) {
-  typedef Shape<T, DH, DUAL, FWD> S;
-  hipLaunchKernelGGL((packed_fwd_kernel<T, DH, S::R, S::NW, S::KB, S::MW, DUAL>),
-                     dim3(a.p.max_tiles[tile_kind(S::R * S::NW)] * a.H), dim3(64 * S::NW), 0, s, a);
+  typedef Shape<T, DH, DUAL, FWD, SMALL> S;
+  hipLaunchKernelGGL((packed_fwd_kernel<T, DH, S::R, S::NW, S::KS, S::KB, S::SB, S::MW, DUAL>),
+                     dim3(a.p.max_tiles[S::KIND] * a.H), dim3(64 * S::NW), 0, s, a);
 }
-template <typename T, int DH, bool DUAL>
+template <typename T, int DH, bool DUAL, bool SMALL>
 hipError_t launch_bwd(const PackedAttnArgs<T>& a, hipStream_t s) {
-  typedef Shape<T, DH, DUAL, DQ> Q;
-  typedef Shape<T, DH, DUAL, DKV> S;
-  hipLaunchKernelGGL((packed_dq_kernel<T, DH, Q::R, Q::NW, Q::KB, Q::MW, DUAL>),
-                     dim3(a.p.max_tiles[tile_kind(Q::R * Q::NW)] * a.H), dim3(64 * Q::NW), 0, s, a);
+  typedef Shape<T, DH, DUAL, DQ, SMALL> Q;
+  typedef Shape<T, DH, DUAL, DKV, SMALL> S;
+  hipLaunchKernelGGL((packed_dq_kernel<T, DH, Q::R, Q::NW, Q::KS, Q::KB, Q::SB, Q::MW, DUAL>),
+                     dim3(a.p.max_tiles[Q::KIND] * a.H), dim3(64 * Q::NW), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((packed_dkv_kernel<T, DH, S::R, S::NW, S::KB, S::MW, DUAL>),
-                     dim3(a.p.max_tiles[tile_kind(S::R * S::NW)] * a.K * a.parts), dim3(64 * S::NW),
-                     0, s, a);
+  hipLaunchKernelGGL((packed_dkv_kernel<T, DH, S::R, S::NW, S::KS, S::KB, S::SB, S::MW, DUAL>),
+                     dim3(a.p.max_tiles[S::KIND] * a.K * a.parts), dim3(64 * S::NW), 0, s, a);
   e = hipGetLastError();
   if (e != hipSuccess || a.parts == 1) return e;
   const long fours = a.p.n * a.K * (a.dual ? 4 : 2) * (a.dh / 4);
   hipLaunchKernelGGL(dkv_sum_kernel<T>, dim3((unsigned)((fours + 255) / 256)), dim3(256), 0, s, a);
   return hipGetLastError();
+}
+
+// Few rows: smaller tiles, so that more workgroups share the work.
+template <typename T>
+bool small(const PackedAttnArgs<T>& a) {
+  return a.p.n * a.H < (sizeof(T) == 4 ? 512 * 64 : 512 * 128);
+}
+template <typename T, int DH>
+hipError_t run(const PackedAttnArgs<T>& a, bool bwd, hipStream_t s) {
+  if (bwd) {
+    if (small(a)) return a.dual ? launch_bwd<T, DH, true, true>(a, s) : launch_bwd<T, DH, false, true>(a, s);
+    return a.dual ? launch_bwd<T, DH, true, false>(a, s) : launch_bwd<T, DH, false, false>(a, s);
+  }
+  if (small(a)) {
+    if (a.dual) launch_fwd<T, DH, true, true>(a, s); else launch_fwd<T, DH, false, true>(a, s);
+  } else {
+    if (a.dual) launch_fwd<T, DH, true, false>(a, s); else launch_fwd<T, DH, false, false>(a, s);
+  }
+  return hipGetLastError();
+}
+// The products' head dimension: dh rounded up to one that is compiled (columns past dh are
+// zero in one operand, or not stored).
+template <typename T>
+hipError_t run_dh(const PackedAttnArgs<T>& a, bool bwd, hipStream_t s) {
+  if (a.dh <= 32) return run<T, 32>(a, bwd, s);
+  if constexpr (sizeof(T) == 4)
+    if (a.dh <= 48) return run<T, 48>(a, bwd, s);
+  if (a.dh <= 64) return run<T, 64>(a, bwd, s);
+  if (a.dh <= 96) return run<T, 96>(a, bwd, s);
+  return run<T, 128>(a, bwd, s);
 }
 
 template <typename T>
@@ -989,10 +1071,10 @@ SeqPlan seq_plan_at(char* base, long n, int m, size_t* bytes) {
   };
   p.n = n;
   p.m = m;
-  p.head = (int*)take(16);
+  p.head = (int*)take(4 * (TILE_KINDS + 2));
   p.bound = (int*)take(4 * ((size_t)m + 1));
   p.pos = (int*)take(4 * (size_t)n);
-  for (int k = 0; k < 2; ++k) {
+  for (int k = 0; k < TILE_KINDS; ++k) {
     p.max_tiles[k] = (int)(n / tile_rows(k) + std::min((long)m, n));
     p.list[k].tstart = (int*)take(4 * ((size_t)m + 1));
     p.list[k].byq = (int4*)take(16 * (size_t)p.max_tiles[k]);
@@ -1027,21 +1109,15 @@ void packed_attn_ws(PackedAttnArgs<T>& a, float* ws) {
 template <typename T>
 hipError_t packed_attn_fwd(const PackedAttnArgs<T>& a, hipStream_t s) {
   if (!shapes_ok(a)) return hipErrorInvalidValue;
-  if (a.p.n < 1 || a.p.max_tiles[0] < 1) return hipSuccess;
-  if (a.dh <= 64) {
-    if (a.dual) launch_fwd<T, 64, true>(a, s); else launch_fwd<T, 64, false>(a, s);
-  } else {
-    if (a.dual) launch_fwd<T, 128, true>(a, s); else launch_fwd<T, 128, false>(a, s);
-  }
-  return hipGetLastError();
+  if (a.p.n < 1 || a.p.m < 1) return hipSuccess;
+  return run_dh(a, false, s);
 }
 
 template <typename T>
 hipError_t packed_attn_bwd(const PackedAttnArgs<T>& a, hipStream_t s) {
   if (!shapes_ok(a)) return hipErrorInvalidValue;
-  if (a.p.n < 1 || a.p.max_tiles[0] < 1) return hipSuccess;
-  if (a.dh <= 64) return a.dual ? launch_bwd<T, 64, true>(a, s) : launch_bwd<T, 64, false>(a, s);
-  return a.dual ? launch_bwd<T, 128, true>(a, s) : launch_bwd<T, 128, false>(a, s);
+  if (a.p.n < 1 || a.p.m < 1) return hipSuccess;
+  return run_dh(a, true, s);
 }
 
 template hipError_t packed_attn_fwd<bf16_t>(const PackedAttnArgs<bf16_t>&, hipStream_t);

@@ -105,7 +105,7 @@ __global__ void __launch_bounds__(64 * WAVES) qk_rope_fwd_kernel(QkRopeArgs<T> a
   const int lane = threadIdx.x & 63, sub = lane / LPH, d = 4 * (lane % LPH);
   const long item = (long)blockIdx.x * WAVES + (threadIdx.x >> 6);
   const long tok = item / splits;
-  if (tok < a.p.head[2] || tok >= a.p.head[3]) return;
+  if (tok < a.p.head[PLAN_FIRST] || tok >= a.p.head[PLAN_LAST]) return;
   const int dh = a.dh, nrot = a.H + a.K, nh = a.H + 2 * a.K;
   const bool live = d < dh;
   const f32x4 none = {0.f, 0.f, 0.f, 0.f};
@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(64 * WAVES) qk_rope_bwd_kernel(QkRopeArgs<T> a
     }
   }
   const float inv = 1.0f / dh;
-  const long first = a.p.head[2], last = a.p.head[3];
+  const long first = a.p.head[PLAN_FIRST], last = a.p.head[PLAN_LAST];
   for (long item = (long)blockIdx.x * WAVES + w; item < a.p.n * splits;
        item += (long)gridDim.x * WAVES) {
     const long tok = item / splits;

@@ -216,3 +216,23 @@ def test_long_rows_pass_32_bit_offsets():
     op.mfmg_attn_fwd(plan, *x.split(cut, 1), o2, stats)
     torch.cuda.synchronize()
     assert torch.equal(o, o2)
+
+
+LARGE = [
+    # enough rows for the large tiles: heads * rows past 512 tiles of 128 (bf16) or 64 (fp32)
+    (32, 4, 64, [700, 129, 1, 640, 63, 600]),
+    (32, 8, 128, [517, 64, 300, 1300]),
+    (36, 12, 96, [1000, 31, 900]),
+    (64, 64, 24, [513, 256, 255, 30]),
+    (44, 11, 40, [800, 777]),
+]
+
+
+@pytest.mark.parametrize("dual", [False, True], ids=["primal", "dual"])
+@pytest.mark.parametrize("prec", [0, 1], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("H,K,dh,lens", LARGE, ids=lambda v: str(v).replace(" ", ""))
+def test_many_rows_against_float64(prec, dual, H, K, dh, lens):
+    print(f"\n[packed] H {H} K {K} dh {dh} lens {lens} prec {prec} dual {dual}", flush=True)
+    c = Call(prec, H, K, dh, lens, dual, before=1, after=9, gap=16).run()
+    torch.cuda.synchronize()
+    c.check()
