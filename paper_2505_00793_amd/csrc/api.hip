@@ -968,7 +968,7 @@ size_t attn_ws_bytes(const mfmg_attn* a, int64_t n) {
   size_t w = 4 * packed_attn_ws_floats(n, a->d.heads, a->d.kv_heads, a->d.head_dim);
   if (a->d.qk_norm && n > 0)
     w = std::max(w, 16 * (size_t)a->d.head_dim *
-                        (size_t)qk_rope_parts(n, a->d.heads, a->d.kv_heads, a->d.head_dim));
+                        (size_t)qk_rope_partials(n, a->d.heads, a->d.kv_heads, a->d.head_dim));
   return (size_t)rup((long)w, 256);
 }
 
@@ -1477,8 +1477,9 @@ mfmg_status run_rope_bwd(QkRopeArgs<T> r, const void* dy, const void* dyd, int64
     P.mode = r.dual ? P_HVP : P_STORE_G;
     P.grad_out = dgain;
     P.hvp_out = dgaind;
-    HIPCHK(gain_param<T>(r.partial, qk_rope_parts(r.p.n, r.H, r.K, r.dh), r.dh, 0, r.dh, P, nullptr,
-                         nullptr, s));
+    int sums = 0;
+    const float* p = qk_rope_sums(r.partial, r.p.n, r.H, r.K, r.dh, &sums);
+    HIPCHK(gain_param<T>(p, sums, r.dh, 0, r.dh, P, nullptr, nullptr, s));
   } else if (r.gain) {
     HIPCHK(fill(dgain, 2 * r.dh, 0.f, s));
     if (r.dual) HIPCHK(fill(dgaind, 2 * r.dh, 0.f, s));

@@ -98,7 +98,7 @@ struct QkRopeArgs {
   T *y, *yd;                      // forward: out.  Backward: y, yd = the cotangent (in),
   T *dx, *dxd;                    //   dx, dxd = the input's gradient (out)
   long ldx, ldxd, ldy, ldyd, lddx, lddxd;
-  float* partial;                 // backward with norms: [qk_rope_parts][4][dh]
+  float* partial;                 // backward with norms: [qk_rope_partials][4][dh]
   SeqPlan p;
   int H, K, dh, dual;
   float eps;
@@ -106,9 +106,11 @@ struct QkRopeArgs {
 };
 template <typename T>
 hipError_t qk_rope_fwd(const QkRopeArgs<T>& a, hipStream_t s);
-// Writes dx (dxd) and, with norms, the partial sums of the gains' gradients
-// (q, k, and their tangents), which gain_param finishes.
-int qk_rope_parts(long n, int H, int K, int dh);
+// Writes dx (dxd) and, with norms, partial sums of the gains' gradients (q, k, and their
+// tangents): qk_rope_partials rows of [4][dh], of which qk_rope_sums says which `count`
+// gain_param finishes.
+int qk_rope_partials(long n, int H, int K, int dh);
+const float* qk_rope_sums(const float* partial, long n, int H, int K, int dh, int* count);
 template <typename T>
 hipError_t qk_rope_bwd(const QkRopeArgs<T>& a, hipStream_t s);
 // The parameter epilogue on column sums of partial [parts][4][d] (transformer.hip).

@@ -39,66 +39,106 @@ __device__ __forceinline__ f32x4 load4(const bf16_t* p) {
 __device__ __forceinline__ float load1(const float* p) { return *p; }
 __device__ __forceinline__ float load1(const bf16_t* p) { return bf2f(*p); }
 
+// Sum over the LPH lanes of a head, in all of them: quads, halves and rows of 16 lanes by
+// DPP (each step adds what the mirrored lane holds of the other half), row pairs by
+// exchanging rows.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+// Lanes 0-15 and 16-31 of each half exchanged.
+__device__ __forceinline__ float swap16(float v) {
+  const unsigned u = __builtin_bit_cast(unsigned, v);
+  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return __builtin_bit_cast(float, (threadIdx.x & 16) ? r[0] : r[1]);
+}
 template <int LPH>
 __device__ __forceinline__ float head_sum(float v) {
-#pragma unroll
-  for (int o = LPH / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  v += dpp<0xb1>(v);    // quad_perm 1 0 3 2
+  v += dpp<0x4e>(v);    // quad_perm 2 3 0 1
+  v += dpp<0x141>(v);   // row_half_mirror
+  if (LPH >= 16) v += dpp<0x140>(v);   // row_mirror
+  if (LPH >= 32) v += swap16(v);
   return v;
 }
 __device__ __forceinline__ float sum4(const f32x4& v) { return (v[0] + v[1]) + (v[2] + v[3]); }
 
-// Rotation of a lane's dims d .. d + 3 of a head at one position: z_k = y_k c_k + y'_k s_k
-// with y' the pairs' other members (back: the transpose has -s).
-struct Rot {
-  f32x4 c, s;
-  int other;    // first dim of y' where the four are consecutive and 4-aligned, else -1
-  int odd[4];   // else their dims
-
-  __device__ __forceinline__ void make(const RopeFreqs& f, int d, int pos) {
-    const int half = f.dims >> 1;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int j = d + k;
-      c[k] = 1.f;
-      s[k] = 0.f;
-      odd[k] = j;
-      if (j < f.dims) {
-        const bool first = f.interleaved ? !(j & 1) : j < half;
-        const int pair = f.interleaved ? j >> 1 : first ? j : j - half;
-        odd[k] = f.interleaved ? j ^ 1 : first ? j + half : j - half;
-        // the angle in quarter turns: k of them and t in [-1/2, 1/2]
-        const double a = (double)pos * f.f4[pair], q = rint(a);
-        float sn, cs;
-        sincospif(0.5f * (float)(a - q), &sn, &cs);
-        const int n = (int)(long long)q & 3;
-        const float cc = n & 1 ? -sn : cs, ss = n & 1 ? cs : sn;
-        const float m = n & 2 ? -f.mscale : f.mscale;
-        c[k] = cc * m;
-        s[k] = first ? -(ss * m) : ss * m;
-      }
-    }
-    other = (odd[0] & 3) == 0 && odd[3] == odd[0] + 3 ? odd[0] : -1;
-  }
-  // the pairs' other members of a head in memory
-  template <typename T>
-  __device__ __forceinline__ f32x4 pairs(const T* head, const f32x4& own, const RopeFreqs& f) const {
-    if (f.interleaved) {   // (a lane's dims are whole pairs; s is 0 past the rotated dims)
-      return f32x4{own[1], own[0], own[3], own[2]};
-    }
-    if ((f.dims & 7) == 0) return load4(head + other);
-    f32x4 v;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = load1(head + odd[k]);
-    return v;
-  }
-};
-
 __device__ __forceinline__ void put4(float* p, const f32x4& v) { store4(p, v[0], v[1], v[2], v[3]); }
 __device__ __forceinline__ void put4(bf16_t* p, const f32x4& v) { store4(p, v[0], v[1], v[2], v[3]); }
 
+// Rotation of a lane's dims d .. d + 3 of a head: z_k = y_k c_k + y'_k s_k with y' the
+// pairs' other members (back: the transpose has -s).
+template <int LPH>
+struct Rot {
+  f32x4 c, s;
+  double f4[4];   // quarter turns per position (0 past the rotated dims)
+  int other[4];   // dims of y'
+  int how;        // where y' is: 0 the lane's own (interleaved), 1 the lane LPH / 2 away
+                  // (the whole head, LPH lanes), 2 four dims in memory, 3 any dims
+  unsigned first; // bit k: dim k is its pair's first member
+
+  __device__ __forceinline__ void init(const RopeFreqs& f, int d) {
+    const int half = f.dims >> 1;
+    how = f.interleaved ? 0 : LPH >= 16 && f.dims == 4 * LPH ? 1 : (f.dims & 7) == 0 ? 2 : 3;
+    first = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int j = d + k;
+      other[k] = j;
+      f4[k] = 0.0;
+      if (j < f.dims) {
+        const bool one = f.interleaved ? !(j & 1) : j < half;
+        other[k] = f.interleaved ? j ^ 1 : one ? j + half : j - half;
+        f4[k] = f.f4[f.interleaved ? j >> 1 : one ? j : j - half];
+        first |= (unsigned)one << k;
+      }
+    }
+  }
+  __device__ __forceinline__ void at(const RopeFreqs& f, int d, int pos) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      // the angle in quarter turns: q of them and the rest, t in [-pi/4, pi/4], by the
+      // power series of sine (to t^9) and cosine (to t^10), exact to 2e-9 there
+      const double a = (double)pos * f4[k], q = rint(a);
+      const float t = (float)(a - q) * 1.57079632679489662f, t2 = t * t;
+      const float sn = t * fmaf(t2, fmaf(t2, fmaf(t2, fmaf(t2, 1.f / 362880, -1.f / 5040), 1.f / 120), -1.f / 6), 1.f);
+      const float cs = fmaf(t2, fmaf(t2, fmaf(t2, fmaf(t2, fmaf(t2, -1.f / 3628800, 1.f / 40320), -1.f / 720),
+                                             1.f / 24), -0.5f), 1.f);
+      const int n = (int)fma(-4.0, floor(0.25 * q), q);   // q mod 4
+      const float cc = n & 1 ? -sn : cs, ss = n & 1 ? cs : sn;
+      const float m = d + k >= f.dims ? 1.f : n & 2 ? -f.mscale : f.mscale;
+      c[k] = cc * m;
+      s[k] = first >> k & 1 ? -(ss * m) : ss * m;
+    }
+  }
+  // y' of a head in memory, where the lanes do not hold it
+  template <typename T>
+  __device__ __forceinline__ f32x4 fetch(const T* head) const {
+    if (how == 2) return load4(head + other[0]);
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (how == 3) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = load1(head + other[k]);
+    }
+    return v;
+  }
+  // y' from the lanes' own values, or as fetched
+  __device__ __forceinline__ f32x4 pairs(const f32x4& own, const f32x4& fetched) const {
+    if (how == 0) return f32x4{own[1], own[0], own[3], own[2]};   // (s is 0 past the rotated dims)
+    if (how == 1) {
+      f32x4 v;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = LPH == 32 ? swap16(own[k]) : dpp<0x128>(own[k]);   // row_ror 8
+      return v;
+    }
+    return fetched;
+  }
+};
+
 // ---------------------------------------------------------------- forward
-// A wave takes every splits-th group of 64 / LPH heads of one token.  Lanes past the
-// head (head dims that are no power of two) hold zeros.
+// A wave takes every splits-th group of 64 / LPH heads of one token, the next group's
+// values requested before the current one's arithmetic.  Lanes past the head (head dims
+// that are no power of two) hold zeros.
 template <typename T, int LPH, bool NORM, bool DUAL>
 __global__ void __launch_bounds__(64 * WAVES) qk_rope_fwd_kernel(QkRopeArgs<T> a, int splits) {
   constexpr int HP = 64 / LPH;
@@ -106,42 +146,62 @@ __global__ void __launch_bounds__(64 * WAVES) qk_rope_fwd_kernel(QkRopeArgs<T> a
   const long item = (long)blockIdx.x * WAVES + (threadIdx.x >> 6);
   const long tok = item / splits;
   if (tok < a.p.head[PLAN_FIRST] || tok >= a.p.head[PLAN_LAST]) return;
-  const int dh = a.dh, nrot = a.H + a.K, nh = a.H + 2 * a.K;
+  const int dh = a.dh, nrot = a.H + a.K, nh = a.H + 2 * a.K, step = splits * HP;
   const bool live = d < dh;
   const f32x4 none = {0.f, 0.f, 0.f, 0.f};
-  Rot rot;
-  rot.make(a.f, d, a.p.pos[tok]);
+  Rot<LPH> rot;
+  rot.init(a.f, d);
+  struct Row {
+    f32x4 v, p, vd, pd;
+  };
+  auto load = [&](int h) {
+    Row r = {none, none, none, none};
+    if (live && h < nh) {
+      const float* x = a.x + tok * a.ldx + (long)h * dh;
+      r.v = load4(x + d);
+      if (rot.how > 1) r.p = rot.fetch(x);
+      if constexpr (DUAL) {
+        const float* xd = a.xd + tok * a.ldxd + (long)h * dh;
+        r.vd = load4(xd + d);
+        if (rot.how > 1) r.pd = rot.fetch(xd);
+      }
+    }
+    return r;
+  };
+  int h = (int)(item % splits) * HP + sub;
+  Row cur = load(h);
+  rot.at(a.f, d, a.p.pos[tok]);
   f32x4 g[2], gp[2], gd[2], gdp[2];   // q, k gains and those of the pairs' other members
   if constexpr (NORM) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       g[k] = live ? load4(a.gain + k * dh + d) : none;
-      gp[k] = live ? rot.pairs(a.gain + k * dh, g[k], a.f) : none;
+      gp[k] = rot.pairs(g[k], live ? rot.fetch(a.gain + k * dh) : none);
       if constexpr (DUAL) {
         gd[k] = live ? load4(a.gaind + k * dh + d) : none;
-        gdp[k] = live ? rot.pairs(a.gaind + k * dh, gd[k], a.f) : none;
+        gdp[k] = rot.pairs(gd[k], live ? rot.fetch(a.gaind + k * dh) : none);
       }
     }
   }
   const float inv = 1.0f / dh;
-  for (int h = (int)(item % splits) * HP + sub; h < nh; h += splits * HP) {
-    const float* x = a.x + tok * a.ldx + (long)h * dh;
-    const float* xd = DUAL ? a.xd + tok * a.ldxd + (long)h * dh : nullptr;
-    f32x4 v = live ? load4(x + d) : none, vd = none;
-    if constexpr (DUAL) vd = live ? load4(xd + d) : none;
+  for (; h < nh; h += step) {
+    const Row next = load(h + step);
+    f32x4 v = cur.v, vd = cur.vd;
     if (h < nrot) {
-      f32x4 p = live ? rot.pairs(x, v, a.f) : none, pd = none;
-      if constexpr (DUAL) pd = live ? rot.pairs(xd, vd, a.f) : none;
+      f32x4 p = rot.pairs(v, cur.p), pd = none;
+      if constexpr (DUAL) pd = rot.pairs(vd, cur.pd);
       if constexpr (NORM) {
-        const int k = h >= a.H;
+        const bool k = h >= a.H;
+        const f32x4 w = k ? g[1] : g[0], wp = k ? gp[1] : gp[0];
         const float r = rsqrtf(head_sum<LPH>(sum4(v * v)) * inv + a.eps);
         if constexpr (DUAL) {
+          const f32x4 wd = k ? gd[1] : gd[0], wdp = k ? gdp[1] : gdp[0];
           const float c = r * head_sum<LPH>(sum4(v * vd)) * inv;
-          vd = gd[k] * (r * v) + g[k] * (r * (vd - c * (r * v)));
-          pd = gdp[k] * (r * p) + gp[k] * (r * (pd - c * (r * p)));
+          vd = wd * (r * v) + w * (r * (vd - c * (r * v)));
+          pd = wdp * (r * p) + wp * (r * (pd - c * (r * p)));
         }
-        v = g[k] * (r * v);
-        p = gp[k] * (r * p);
+        v = w * (r * v);
+        p = wp * (r * p);
       }
       v = v * rot.c + p * rot.s;
       if constexpr (DUAL) vd = vd * rot.c + pd * rot.s;
@@ -150,6 +210,7 @@ __global__ void __launch_bounds__(64 * WAVES) qk_rope_fwd_kernel(QkRopeArgs<T> a
       put4(a.y + tok * a.ldy + (long)h * dh + d, v);
       if constexpr (DUAL) put4(a.yd + tok * a.ldyd + (long)h * dh + d, vd);
     }
+    cur = next;
   }
 }
 
@@ -161,9 +222,9 @@ template <typename T, int LPH, bool NORM, bool DUAL>
 __global__ void __launch_bounds__(64 * WAVES) qk_rope_bwd_kernel(QkRopeArgs<T> a, int splits) {
   constexpr int HP = 64 / LPH, NA = NORM ? (DUAL ? 4 : 2) : 0;
   __shared__ float red[NORM ? WAVES * HP * 4 * 4 * LPH : 1];
-  const int lane = threadIdx.x & 63, sub = lane / LPH, i = lane % LPH, d = 4 * i;
+  const int lane = threadIdx.x & 63, sub = lane / LPH, d = 4 * (lane % LPH);
   const int w = threadIdx.x >> 6;
-  const int dh = a.dh, nrot = a.H + a.K, nh = a.H + 2 * a.K;
+  const int dh = a.dh, nrot = a.H + a.K, nh = a.H + 2 * a.K, step = splits * HP;
   const bool live = d < dh;
   const f32x4 none = {0.f, 0.f, 0.f, 0.f};
   f32x4 acc[NORM ? 4 : 1];   // q, k gains' gradients, then their tangents
@@ -179,46 +240,67 @@ __global__ void __launch_bounds__(64 * WAVES) qk_rope_bwd_kernel(QkRopeArgs<T> a
   }
   const float inv = 1.0f / dh;
   const long first = a.p.head[PLAN_FIRST], last = a.p.head[PLAN_LAST];
+  Rot<LPH> rot;
+  rot.init(a.f, d);
+  struct Row {
+    f32x4 v, p, vd, pd, x, xd;
+  };
   for (long item = (long)blockIdx.x * WAVES + w; item < a.p.n * splits;
        item += (long)gridDim.x * WAVES) {
     const long tok = item / splits;
     if (tok < first || tok >= last) continue;
-    Rot rot;
-    rot.make(a.f, d, a.p.pos[tok]);
-    for (int h = (int)(item % splits) * HP + sub; h < nh; h += splits * HP) {
-      const long col = (long)h * dh;
-      const T* y = a.y + tok * a.ldy + col;
-      const T* yd = DUAL ? a.yd + tok * a.ldyd + col : nullptr;
-      f32x4 v = live ? load4(y + d) : none, vd = none;
-      if constexpr (DUAL) vd = live ? load4(yd + d) : none;
-      if (h < nrot) {
-        v = v * rot.c - (live ? rot.pairs(y, v, a.f) : none) * rot.s;
-        if constexpr (DUAL) vd = vd * rot.c - (live ? rot.pairs(yd, vd, a.f) : none) * rot.s;
+    auto load = [&](int h) {
+      Row r = {none, none, none, none, none, none};
+      if (live && h < nh) {
+        const T* y = a.y + tok * a.ldy + (long)h * dh;
+        r.v = load4(y + d);
+        if (rot.how > 1) r.p = rot.fetch(y);
+        if constexpr (DUAL) {
+          const T* yd = a.yd + tok * a.ldyd + (long)h * dh;
+          r.vd = load4(yd + d);
+          if (rot.how > 1) r.pd = rot.fetch(yd);
+        }
         if constexpr (NORM) {
-          const int k = h >= a.H;
-          const f32x4 x = live ? load4(a.x + tok * a.ldx + col + d) : none;
-          const f32x4 e = g[k] * v;
-          const float r = rsqrtf(head_sum<LPH>(sum4(x * x)) * inv + a.eps);
-          const float m = r * head_sum<LPH>(sum4(x * e)) * inv;
-          const f32x4 xh = r * x;
-          const f32x4 u = e - m * xh;
-          acc[k] += v * xh;
+          if (h < nrot) {
+            r.x = load4(a.x + tok * a.ldx + (long)h * dh + d);
+            if constexpr (DUAL) r.xd = load4(a.xd + tok * a.ldxd + (long)h * dh + d);
+          }
+        }
+      }
+      return r;
+    };
+    int h = (int)(item % splits) * HP + sub;
+    Row cur = load(h);
+    rot.at(a.f, d, a.p.pos[tok]);
+    for (; h < nh; h += step) {
+      const Row next = load(h + step);
+      f32x4 v = cur.v, vd = cur.vd;
+      if (h < nrot) {
+        v = v * rot.c - rot.pairs(v, cur.p) * rot.s;
+        if constexpr (DUAL) vd = vd * rot.c - rot.pairs(vd, cur.pd) * rot.s;
+        if constexpr (NORM) {
+          const bool k = h >= a.H;
+          const f32x4 e = (k ? g[1] : g[0]) * v;
+          const float r = rsqrtf(head_sum<LPH>(sum4(cur.x * cur.x)) * inv + a.eps);
+          const float m = r * head_sum<LPH>(sum4(cur.x * e)) * inv;
+          const f32x4 xh = r * cur.x, u = e - m * xh, dg = v * xh;
+          if (k) acc[1] += dg; else acc[0] += dg;
           if constexpr (DUAL) {
-            const f32x4 xd = live ? load4(a.xd + tok * a.ldxd + col + d) : none;
-            const f32x4 ed = gd[k] * v + g[k] * vd;
-            const float c = r * head_sum<LPH>(sum4(x * xd)) * inv;
-            const f32x4 xhd = r * (xd - c * xh);
+            const f32x4 ed = (k ? gd[1] : gd[0]) * v + (k ? g[1] : g[0]) * vd;
+            const float c = r * head_sum<LPH>(sum4(cur.x * cur.xd)) * inv;
+            const f32x4 xhd = r * (cur.xd - c * xh), dgd = vd * xh + v * xhd;
             const float md = head_sum<LPH>(sum4(xhd * e + xh * ed)) * inv;
-            acc[2 + k] += vd * xh + v * xhd;
+            if (k) acc[3] += dgd; else acc[2] += dgd;
             vd = (-r * r * c) * u + r * (ed - m * xhd - md * xh);
           }
           v = r * u;
         }
       }
       if (live) {
-        put4(a.dx + tok * a.lddx + col + d, v);
-        if constexpr (DUAL) put4(a.dxd + tok * a.lddxd + col + d, vd);
+        put4(a.dx + tok * a.lddx + (long)h * dh + d, v);
+        if constexpr (DUAL) put4(a.dxd + tok * a.lddxd + (long)h * dh + d, vd);
       }
+      cur = next;
     }
   }
   if constexpr (NORM) {
@@ -237,6 +319,26 @@ __global__ void __launch_bounds__(64 * WAVES) qk_rope_bwd_kernel(QkRopeArgs<T> a
   }
 }
 
+// Partials in groups of GROUP consecutive ones, added in order: [parts][4][dh] ->
+// [cdiv(parts, GROUP)][4][dh] behind them.
+constexpr int GROUP = 32;
+__global__ void __launch_bounds__(256) gain_group_kernel(const float* __restrict__ partial, int parts,
+                                                         int cols, float* __restrict__ out) {
+  __shared__ float red[4][64];
+  const int c = threadIdx.x & 63, ph = threadIdx.x >> 6, j = blockIdx.x * 64 + c;
+  const int p0 = blockIdx.y * GROUP + ph * (GROUP / 4);
+  float v[GROUP / 4];
+#pragma unroll
+  for (int k = 0; k < GROUP / 4; ++k)
+    v[k] = j < cols && p0 + k < parts ? partial[(long)(p0 + k) * cols + j] : 0.f;
+  float s = 0.f;
+#pragma unroll
+  for (int k = 0; k < GROUP / 4; ++k) s += v[k];
+  red[ph][c] = s;
+  __syncthreads();
+  if (ph == 0 && j < cols) out[(long)blockIdx.y * cols + j] = (red[0][c] + red[1][c]) + (red[2][c] + red[3][c]);
+}
+
 int lanes_per_head(int dh) { return dh <= 32 ? 8 : dh <= 64 ? 16 : 32; }
 
 // Waves of one token: its groups of heads are dealt to more waves while there are too
@@ -247,17 +349,29 @@ int splits_of(long n, int H, int K, int dh) {
   while (s < groups && n * s < 8192) s *= 2;
   return std::min(s, groups);
 }
-int bwd_blocks(long n, int H, int K, int dh) {
+int bwd_blocks(long n, int H, int K, int dh) {   // (with norms)
   const long items = n * splits_of(n, H, K, dh);
   return (int)std::min((long)MAX_PARTS, std::max(1L, (items + WAVES - 1) / WAVES));
 }
+
+// Few partials are left as they are.
+int gain_groups(int parts) { return parts <= GROUP ? parts : (parts + GROUP - 1) / GROUP; }
 
 template <typename T, int LPH, bool NORM, bool DUAL>
 hipError_t launch(const QkRopeArgs<T>& a, bool bwd, hipStream_t s) {
   const int splits = splits_of(a.p.n, a.H, a.K, a.dh);
   if (bwd) {
-    hipLaunchKernelGGL((qk_rope_bwd_kernel<T, LPH, NORM, DUAL>),
-                       dim3(bwd_blocks(a.p.n, a.H, a.K, a.dh)), dim3(64 * WAVES), 0, s, a, splits);
+    const int blocks = NORM ? bwd_blocks(a.p.n, a.H, a.K, a.dh)
+                            : (int)((a.p.n * splits + WAVES - 1) / WAVES);
+    hipLaunchKernelGGL((qk_rope_bwd_kernel<T, LPH, NORM, DUAL>), dim3(blocks), dim3(64 * WAVES), 0,
+                       s, a, splits);
+    const int groups = gain_groups(blocks);
+    if (NORM && groups < blocks) {
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      hipLaunchKernelGGL(gain_group_kernel, dim3((4 * a.dh + 63) / 64, groups), dim3(256), 0, s,
+                         a.partial, blocks, 4 * a.dh, a.partial + (long)blocks * 4 * a.dh);
+    }
   } else {
     const long blocks = (a.p.n * splits + WAVES - 1) / WAVES;
     hipLaunchKernelGGL((qk_rope_fwd_kernel<T, LPH, NORM, DUAL>), dim3((unsigned)blocks),
@@ -337,7 +451,15 @@ RopeFreqs rope_freqs(const mfmg_attn_desc& d) {
   return f;
 }
 
-int qk_rope_parts(long n, int H, int K, int dh) { return bwd_blocks(n, H, K, dh); }
+int qk_rope_partials(long n, int H, int K, int dh) {
+  const int parts = bwd_blocks(n, H, K, dh);
+  return parts + gain_groups(parts);
+}
+const float* qk_rope_sums(const float* partial, long n, int H, int K, int dh, int* count) {
+  const int parts = bwd_blocks(n, H, K, dh);
+  *count = gain_groups(parts);
+  return *count < parts ? partial + (long)parts * 4 * dh : partial;
+}
 
 template <typename T>
 hipError_t qk_rope_fwd(const QkRopeArgs<T>& a, hipStream_t s) { return launch_heads(a, false, s); }

@@ -342,8 +342,8 @@ void carve_act_bufs(const Lay& y, Carver& c, Act<T>& a, int sets, bool all) {
     a.dY = OPT(N * y.ld(y.QC)); a.dYd = OPT(N * y.ld(y.QC));
     if (y.norm) {
       // (parts do not grow steadily with the rows)
-      const int parts = std::max(qk_rope_parts((long)y.Bt * S, y.H, y.K, y.dh),
-                                 qk_rope_parts((long)y.Bv * S, y.H, y.K, y.dh));
+      const int parts = std::max(qk_rope_partials((long)y.Bt * S, y.H, y.K, y.dh),
+                                 qk_rope_partials((long)y.Bv * S, y.H, y.K, y.dh));
       a.qkpart = F32((long)parts * 4 * y.dh);
     }
     size_t pt = 0, pv = 0;
@@ -1018,9 +1018,12 @@ struct TfEng {
         r.y = a.dY; r.yd = a.dYd;
         r.dx = a.dZ1; r.dxd = a.dZ1d;
         HC(qk_rope_bwd(r, s));
-        if (y.norm)
-          HC(gain_param<T>(a.qkpart, qk_rope_parts(N, H, y.K, dh), dh, y.qkg[b], y.qkg[b] + dh, P,
-                           out ? out->qk[b] : nullptr, out ? out->qk[b] + dh : nullptr, s));
+        if (y.norm) {
+          int sums = 0;
+          const float* p = qk_rope_sums(a.qkpart, N, H, y.K, dh, &sums);
+          HC(gain_param<T>(p, sums, dh, y.qkg[b], y.qkg[b] + dh, P, out ? out->qk[b] : nullptr,
+                           out ? out->qk[b] + dh : nullptr, s));
+        }
         HC(packed_copy(a.dZ1, dual ? a.dZ1d : nullptr, N, y.QC, a.dZ1T, a.dZ1dT));
       } else if (y.fused) {
         HC(attn_bwd(attn_args(b, Bn, dual, a), s));
