@@ -139,46 +139,63 @@ __device__ __forceinline__ f32x4 gfrag(const float* p, int g, int c, int dh) {
   return d < dh ? *reinterpret_cast<const f32x4*>(p + d) : f32x4{0.f, 0.f, 0.f, 0.f};
 }
 
-// The same of row row0 + row of an LDS tile (row0 a multiple of 16, which leaves the
-// swizzle alone).
-template <typename T, int DH, int NG>
-__device__ __forceinline__ typename FragT<T>::V frag(const T* lds, int row0, int row, int g, int c) {
-  typedef Tile<T, DH> L;
-  return *reinterpret_cast<const typename FragT<T>::V*>(lds + L::at(row, NG * c + g) + row0 * L::P);
-}
-
-// Fragment c of column R e + (lane % R) of an LDS tile: rows idx(FE c + t), t < FE.
-// ds_read_b64_tr_b16 works on groups of 16 lanes: lane i reads 4 elements at its own
-// address and lane j gets element j % 4 of lanes j / 4, j / 4 + 4, + 8, + 12, so with
-// lane i at row i / 4 and columns 4 (i % 4) .. + 3, lane j holds 4 rows of column j.
+// Where a lane finds its parts of an LDS tile.  frag: fragment c of row row0 + lane % R
+// (row0 a multiple of 16, which leaves the swizzle alone).  tfrag: fragment c of column
+// R e + lane % R, rows idx(FE c + t), t < FE.  The chunk indices are XORed with the
+// swizzle, so the address of another c or e is one XOR away from the first: `pin` hides
+// the bases from the compiler, which would otherwise keep every address in a register
+// of its own through the whole loop.
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4s lds_v4s;
+template <typename T, int DH, int R>
+struct Lane;
 template <int DH, int R>
-__device__ __forceinline__ bf16x8 tfrag(const bf16_t* lds, int e, int lane, int c) {
-  constexpr int NG = 64 / R;
+struct Lane<bf16_t, DH, R> {
   typedef Tile<bf16_t, DH> L;
-  const int g = lane / R, i = lane & 15, sub = (lane % R) >> 4;
-  const int row = 4 * g + (i >> 2), ch = (e * R + 16 * sub) / 8 + ((i >> 1) & 1);
-  const bf16_t* p = lds + L::at(row, ch) + (i & 1) * 4 + 8 * NG * c * L::P;
-  const bf16_t* q = lds + L::at(row + 4 * NG, ch) + (i & 1) * 4 + 8 * NG * c * L::P;
-  union {
-    v4s h[2];
-    bf16x8 v;
-  } x;
-  x.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)p);
-  x.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)q);
-  return x.v;
-}
+  static constexpr int NG = 64 / R;
+  int f, t0, t1;
+  // ds_read_b64_tr_b16 works on groups of 16 lanes: lane i reads 4 elements at its own
+  // address and lane j gets element j % 4 of lanes j / 4, j / 4 + 4, + 8, + 12, so with
+  // lane i at row i / 4 and columns 4 (i % 4) .. + 3, lane j holds 4 rows of column j.
+  __device__ __forceinline__ Lane(int lane) {
+    const int g = lane / R, i = lane & 15, sub = (lane % R) >> 4;
+    const int row = 4 * g + (i >> 2), ch = 2 * sub + ((i >> 1) & 1);
+    f = L::at(lane % R, g);
+    t0 = L::at(row, ch) + (i & 1) * 4;
+    t1 = L::at(row + 4 * NG, ch) + (i & 1) * 4;
+  }
+  __device__ __forceinline__ void pin() { asm volatile("" : "+v"(f), "+v"(t0), "+v"(t1)); }
+  __device__ __forceinline__ bf16x8 frag(const bf16_t* lds, int row0, int c) const {
+    return *reinterpret_cast<const bf16x8*>(lds + (f ^ (8 * NG * c)) + row0 * L::P);
+  }
+  __device__ __forceinline__ bf16x8 tfrag(const bf16_t* lds, int e, int c) const {
+    union {
+      v4s h[2];
+      bf16x8 v;
+    } x;
+    x.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(lds + (t0 ^ (R * e)) + 8 * NG * c * L::P));
+    x.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(lds + (t1 ^ (R * e)) + 8 * NG * c * L::P));
+    return x.v;
+  }
+};
 template <int DH, int R>
-__device__ __forceinline__ f32x4 tfrag(const float* lds, int e, int lane, int c) {
-  constexpr int NG = 64 / R;
+struct Lane<float, DH, R> {
   typedef Tile<float, DH> L;
-  const int g = lane / R, col = e * R + lane % R;
-  f32x4 v;
+  static constexpr int NG = 64 / R;
+  int g, r;
+  __device__ __forceinline__ Lane(int lane) : g(lane / R), r(lane % R) {}
+  __device__ __forceinline__ void pin() {}
+  __device__ __forceinline__ f32x4 frag(const float* lds, int row0, int c) const {
+    return *reinterpret_cast<const f32x4*>(lds + L::at(r, NG * c + g) + row0 * L::P);
+  }
+  __device__ __forceinline__ f32x4 tfrag(const float* lds, int e, int c) const {
+    const int col = e * R + r;
+    f32x4 v;
 #pragma unroll
-  for (int t = 0; t < 4; ++t) v[t] = lds[L::at(4 * g + t, col / 4) + (col & 3) + 4 * NG * c * L::P];
-  return v;
-}
+    for (int t = 0; t < 4; ++t) v[t] = lds[L::at(4 * g + t, col / 4) + (col & 3) + 4 * NG * c * L::P];
+    return v;
+  }
+};
 
 // Fragment c from the lane's own values (flat index FE c .. + FE - 1).  bf16 rounds P and
 // the score cotangents to nearest even: the products take bf16 operands, and the softmax
@@ -272,7 +289,7 @@ __device__ __forceinline__ void tile_of(int heads, int& rank, int& head) {
 // more than 2^8: until then exp2 stays below 2^8 times its usual range, far from
 // float32's, and a factor common to numerator and denominator changes neither's
 // relative error.
-template <typename T, int DH, int R, int NW, int KS, int KB, int SB, int MW, bool DUAL>
+template <typename T, int DH, int R, int NW, int KS, int KB, int SB, int MW, bool PIN, bool DUAL>
 __global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<T> a) {
   constexpr int NT = 64 * NW, NG = 64 / R, NS = SB / R, NE = DH / R, FE = FragT<T>::FE, NC = DH / (FE * NG);
   constexpr int AV = R * R / 64, NK = SB / (FE * NG), ROWS = NW * R / KS;
@@ -289,6 +306,7 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<
   const int lo = tile.y, hi = tile.z;
   const int tid = threadIdx.x, lane = tid & 63, lr = lane % R, g = lane / R;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  Lane<T, DH, R> at(lane);
   const int q0 = tile.x + w / KS * R, q = q0 + lr, qc = min(q, hi - 1);
   const int kh = h / (a.H / a.K), dh = a.dh;
   const T* K = a.k + (long)kh * dh;
@@ -345,6 +363,7 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<
       const int ks = k0 + sb * SB;
       if (KS > 1 && sb % KS != w % KS) continue;
       if (ks > q0 + R - 1 || q0 >= hi) break;   // nothing further is visible to the wave
+      if constexpr (PIN) at.pin();
       V s[NS], sd[DUAL ? NS : 1];
 #pragma unroll
       for (int n = 0; n < NS; ++n) {
@@ -352,11 +371,11 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<
         if constexpr (DUAL) zero(sd[n]);
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-          const F kf = frag<T, DH, NG>(sK[b], sb * SB + n * R, lr, g, c);
+          const F kf = at.frag(sK[b], sb * SB + n * R, c);
           s[n] = mma(kf, qf[c], s[n]);
           if constexpr (DUAL) {
             sd[n] = mma(kf, qdf[c], sd[n]);
-            sd[n] = mma(frag<T, DH, NG>(sKd[b], sb * SB + n * R, lr, g, c), qf[c], sd[n]);
+            sd[n] = mma(at.frag(sKd[b], sb * SB + n * R, c), qf[c], sd[n]);
           }
         }
       }
@@ -401,11 +420,11 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<
         if constexpr (DUAL) pack(sd, c, pdf);
 #pragma unroll
         for (int e = 0; e < NE; ++e) {
-          const F vf = tfrag<DH, R>(sV[b], e, lane, sb * NK + c);
+          const F vf = at.tfrag(sV[b], e, sb * NK + c);
           o[e] = mma(vf, pf, o[e]);
           if constexpr (DUAL) {
             od[e] = mma(vf, pdf, od[e]);
-            od[e] = mma(tfrag<DH, R>(sVd[b], e, lane, sb * NK + c), pf, od[e]);
+            od[e] = mma(at.tfrag(sVd[b], e, sb * NK + c), pf, od[e]);
           }
         }
       }
@@ -467,7 +486,7 @@ __device__ __forceinline__ float dot(const f32x4& a, const f32x4& b) {
 }
 
 // Scores' cotangents are formed without the scale s, which the sums take at the end.
-template <typename T, int DH, int R, int NW, int KS, int KB, int SB, int MW, bool DUAL>
+template <typename T, int DH, int R, int NW, int KS, int KB, int SB, int MW, bool PIN, bool DUAL>
 __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T> a) {
   constexpr int NT = 64 * NW, NG = 64 / R, NS = SB / R, NE = DH / R, FE = FragT<T>::FE, NC = DH / (FE * NG);
   constexpr int AV = R * R / 64, NK = SB / (FE * NG), ROWS = NW * R / KS;
@@ -484,6 +503,7 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T
   const int lo = tile.y, hi = tile.z;
   const int tid = threadIdx.x, lane = tid & 63, lr = lane % R, g = lane / R;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  Lane<T, DH, R> at(lane);
   const int q0 = tile.x + w / KS * R, q = q0 + lr, qc = min(q, hi - 1);
   const int kh = h / (a.H / a.K), dh = a.dh;
   const T* K = a.k + (long)kh * dh;
@@ -556,6 +576,7 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T
       const int ks = k0 + sb * SB;
       if (KS > 1 && sb % KS != w % KS) continue;
       if (ks > q0 + R - 1 || q0 >= hi) break;
+      if constexpr (PIN) at.pin();
       const bool diag = ks + SB - 1 > q0;
       V ds[NS], dsd[DUAL ? NS : 1];
 #pragma unroll
@@ -565,14 +586,14 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
           const int kr = sb * SB + n * R;
-          const F kf = frag<T, DH, NG>(sK[b], kr, lr, g, c), vf = frag<T, DH, NG>(sV[b], kr, lr, g, c);
+          const F kf = at.frag(sK[b], kr, c), vf = at.frag(sV[b], kr, c);
           s = mma(kf, qf[c], s);
           dp = mma(vf, gf[c], dp);
           if constexpr (DUAL) {
             sd = mma(kf, qdf[c], sd);
-            sd = mma(frag<T, DH, NG>(sKd[b], kr, lr, g, c), qf[c], sd);
+            sd = mma(at.frag(sKd[b], kr, c), qf[c], sd);
             dpd = mma(vf, gdf[c], dpd);
-            dpd = mma(frag<T, DH, NG>(sVd[b], kr, lr, g, c), gf[c], dpd);
+            dpd = mma(at.frag(sVd[b], kr, c), gf[c], dpd);
           }
         }
         if (diag) {   // some key may follow some query: its weight is 2^-inf = 0
@@ -598,11 +619,11 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T
         if constexpr (DUAL) pack(dsd, c, ddf);
 #pragma unroll
         for (int e = 0; e < NE; ++e) {
-          const F kt = tfrag<DH, R>(sK[b], e, lane, sb * NK + c);
+          const F kt = at.tfrag(sK[b], e, sb * NK + c);
           dq[e] = mma(kt, df, dq[e]);
           if constexpr (DUAL) {
             dqd[e] = mma(kt, ddf, dqd[e]);
-            dqd[e] = mma(tfrag<DH, R>(sKd[b], e, lane, sb * NK + c), df, dqd[e]);
+            dqd[e] = mma(at.tfrag(sKd[b], e, sb * NK + c), df, dqd[e]);
           }
         }
       }
@@ -629,7 +650,7 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T
 // A workgroup owns NW R keys of one key head and goes through the queries of some of the
 // head's query heads (all, or one part of `parts`, whose float32 sums dkv_sum_kernel
 // adds in order).
-template <typename T, int DH, int R, int NW, int KS, int KB, int SB, int MW, bool DUAL>
+template <typename T, int DH, int R, int NW, int KS, int KB, int SB, int MW, bool PIN, bool DUAL>
 __global__ void __launch_bounds__(64 * NW, MW) packed_dkv_kernel(PackedAttnArgs<T> a) {
   constexpr int NT = 64 * NW, NG = 64 / R, NS = SB / R, NE = DH / R, FE = FragT<T>::FE, NC = DH / (FE * NG);
   constexpr int AV = R * R / 64, NK = SB / (FE * NG), ROWS = NW * R / KS;
@@ -647,6 +668,7 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dkv_kernel(PackedAttnArgs<
   const int kh = hp / a.parts, part = hp - kh * a.parts, hi = tile.z;
   const int tid = threadIdx.x, lane = tid & 63, lr = lane % R, g = lane / R;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  Lane<T, DH, R> at(lane);
   const int k0 = tile.x + w / KS * R, k = k0 + lr, kc = min(k, hi - 1);
   const int GP = a.H / a.K / a.parts, dh = a.dh;   // query heads of a part
   const int h0 = (kh * a.parts + part) * GP;
@@ -724,6 +746,7 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dkv_kernel(PackedAttnArgs<
       const int qs = r0 + sb * SB;
       if (KS > 1 && sb % KS != w % KS) continue;
       if (qs + SB - 1 < k0 || k0 >= hi || qs >= hi) continue;   // no query of these sees the wave's keys
+      if constexpr (PIN) at.pin();
       const bool mask = qs < k0 + R - 1 || qs + SB > hi;
       V p[NS], ds[NS], pd[DUAL ? NS : 1], dsd[DUAL ? NS : 1];
 #pragma unroll
@@ -733,14 +756,14 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dkv_kernel(PackedAttnArgs<
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
           const int qr = sb * SB + n * R;
-          const F qq = frag<T, DH, NG>(sQ[b], qr, lr, g, c), gg = frag<T, DH, NG>(sG[b], qr, lr, g, c);
+          const F qq = at.frag(sQ[b], qr, c), gg = at.frag(sG[b], qr, c);
           s = mma(qq, kf[c], s);
           dp = mma(gg, vf[c], dp);
           if constexpr (DUAL) {
             sd = mma(qq, kdf[c], sd);
-            sd = mma(frag<T, DH, NG>(sQd[b], qr, lr, g, c), kf[c], sd);
+            sd = mma(at.frag(sQd[b], qr, c), kf[c], sd);
             dpd = mma(gg, vdf[c], dpd);
-            dpd = mma(frag<T, DH, NG>(sGd[b], qr, lr, g, c), vf[c], dpd);
+            dpd = mma(at.frag(sGd[b], qr, c), vf[c], dpd);
           }
         }
         if (mask) {   // (weight 0, as above)
@@ -785,15 +808,15 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dkv_kernel(PackedAttnArgs<
         }
 #pragma unroll
         for (int e = 0; e < NE; ++e) {
-          const F gt = tfrag<DH, R>(sG[b], e, lane, sb * NK + c);
-          const F qt = tfrag<DH, R>(sQ[b], e, lane, sb * NK + c);
+          const F gt = at.tfrag(sG[b], e, sb * NK + c);
+          const F qt = at.tfrag(sQ[b], e, sb * NK + c);
           dv[e] = mma(gt, pf, dv[e]);
           dk[e] = mma(qt, df, dk[e]);
           if constexpr (DUAL) {
             dvd[e] = mma(gt, pdf, dvd[e]);
-            dvd[e] = mma(tfrag<DH, R>(sGd[b], e, lane, sb * NK + c), pf, dvd[e]);
+            dvd[e] = mma(at.tfrag(sGd[b], e, sb * NK + c), pf, dvd[e]);
             dkd[e] = mma(qt, ddf, dkd[e]);
-            dkd[e] = mma(tfrag<DH, R>(sQd[b], e, lane, sb * NK + c), df, dkd[e]);
+            dkd[e] = mma(at.tfrag(sQd[b], e, sb * NK + c), df, dkd[e]);
           }
         }
       }
@@ -986,7 +1009,21 @@ int dkv_parts(long n, int H, int K) {
 }
 
 // Rows a wave owns, waves of a workgroup, waves that share rows, rows of a staged block, rows
-// of it that a wave forms and consumes scores of at a time, waves a SIMD holds.
+// of it that a wave forms and consumes scores of at a time, waves a SIMD holds, addresses
+// pinned (Lane).  What they were chosen by, in us:
+//  forward and dQ, 128 dims, bf16 (16 x 400 tokens of 16 heads | 16384 tokens): 32 rows a
+//   wave, 4 waves, 104 | 1160 and 170; 16 rows, 4 waves 115 | 1380 and 178 (twice the LDS
+//   reads a product); 16 rows, 8 waves 110 | 1200 and 200;
+//  dK/dV, 128 dims: 16 rows, 4 waves 209; 16 rows, 8 waves 246; 32 rows need more
+//   registers than two waves a SIMD have (593 with spills, 246 with V in LDS);
+//  dual, 64 dims (2 x 4096 tokens of 8 heads): 16 rows, 8 waves 131, 167, 226 for the three
+//   passes; 4 waves 135, 193, 257; 32 rows 145, 232, 277;
+//  dual, 128 dims (8191 tokens of 12 heads): 16 rows, 4 waves, blocks of 32 and one wave a
+//   SIMD for dK/dV 165, 225, 379; 8 waves 165, 238, 1340 (spills); unpinned 165, 250, 410;
+//  float32: 16 rows, one wave a SIMD (dual 64 dims: 32 rows take twice the time);
+//  few rows (bf16: 16 x 256 tokens of 8 heads, 64-row tiles 8.1, 9.6, 10.5, 128-row tiles 9.0,
+//   11.4, 15.4; float32: 1531 tokens of 6 heads, pairs of waves sharing 32 rows 62, 79, 105,
+//   64-row tiles 118, 166, 229).
 enum Pass { FWD, DQ, DKV };
 template <typename T, int DH, bool DUAL, int PASS, bool SMALL>
 struct Shape {
@@ -994,27 +1031,28 @@ struct Shape {
   static constexpr int R = !F32 && !DUAL && PASS != DKV && !SMALL ? 32 : 16;
   static constexpr int NW = !F32 && DUAL && !BIG && !SMALL ? 8 : 4;
   static constexpr int KS = F32 && SMALL ? 2 : 1;
-  static constexpr int KB = BIG && DUAL && (F32 || PASS != DKV) ? 32 : 64;
+  static constexpr int KB = BIG && (DUAL ? F32 || PASS != DKV : !F32 && PASS == FWD) ? 32 : 64;
   static constexpr int SB = KB == 32 && KS == 2 ? 16 : 32;
   static constexpr int MW = F32 || (DUAL && BIG && PASS == DKV) ? 1 : 2;
+  static constexpr bool PIN = !F32 && BIG && (DUAL ? PASS != FWD : PASS == FWD);
   static constexpr int KIND = tile_kind(NW * R / KS);
 };
 
 template <typename T, int DH, bool DUAL, bool SMALL>
 void launch_fwd(const PackedAttnArgs<T>& a, hipStream_t s) {
   typedef Shape<T, DH, DUAL, FWD, SMALL> S;
-  hipLaunchKernelGGL((packed_fwd_kernel<T, DH, S::R, S::NW, S::KS, S::KB, S::SB, S::MW, DUAL>),
+  hipLaunchKernelGGL((packed_fwd_kernel<T, DH, S::R, S::NW, S::KS, S::KB, S::SB, S::MW, S::PIN, DUAL>),
                      dim3(a.p.max_tiles[S::KIND] * a.H), dim3(64 * S::NW), 0, s, a);
 }
 template <typename T, int DH, bool DUAL, bool SMALL>
 hipError_t launch_bwd(const PackedAttnArgs<T>& a, hipStream_t s) {
   typedef Shape<T, DH, DUAL, DQ, SMALL> Q;
   typedef Shape<T, DH, DUAL, DKV, SMALL> S;
-  hipLaunchKernelGGL((packed_dq_kernel<T, DH, Q::R, Q::NW, Q::KS, Q::KB, Q::SB, Q::MW, DUAL>),
+  hipLaunchKernelGGL((packed_dq_kernel<T, DH, Q::R, Q::NW, Q::KS, Q::KB, Q::SB, Q::MW, Q::PIN, DUAL>),
                      dim3(a.p.max_tiles[Q::KIND] * a.H), dim3(64 * Q::NW), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((packed_dkv_kernel<T, DH, S::R, S::NW, S::KS, S::KB, S::SB, S::MW, DUAL>),
+  hipLaunchKernelGGL((packed_dkv_kernel<T, DH, S::R, S::NW, S::KS, S::KB, S::SB, S::MW, S::PIN, DUAL>),
                      dim3(a.p.max_tiles[S::KIND] * a.K * a.parts), dim3(64 * S::NW), 0, s, a);
   e = hipGetLastError();
   if (e != hipSuccess || a.parts == 1) return e;
