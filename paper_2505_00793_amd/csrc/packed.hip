@@ -182,18 +182,24 @@ template <int DH, int R>
 struct Lane<float, DH, R> {
   typedef Tile<float, DH> L;
   static constexpr int NG = 64 / R;
-  int g, r;
-  __device__ __forceinline__ Lane(int lane) : g(lane / R), r(lane % R) {}
-  __device__ __forceinline__ void pin() {}
+  int f, t0, t1, t2, t3;   // (a lane's four rows of a column are swizzled differently)
+  __device__ __forceinline__ Lane(int lane) {
+    const int g = lane / R, r = lane % R;
+    f = L::at(r, g);
+    t0 = L::at(4 * g, r / 4) + (r & 3);
+    t1 = L::at(4 * g + 1, r / 4) + (r & 3);
+    t2 = L::at(4 * g + 2, r / 4) + (r & 3);
+    t3 = L::at(4 * g + 3, r / 4) + (r & 3);
+  }
+  __device__ __forceinline__ void pin() {
+    asm volatile("" : "+v"(f), "+v"(t0), "+v"(t1), "+v"(t2), "+v"(t3));
+  }
   __device__ __forceinline__ f32x4 frag(const float* lds, int row0, int c) const {
-    return *reinterpret_cast<const f32x4*>(lds + L::at(r, NG * c + g) + row0 * L::P);
+    return *reinterpret_cast<const f32x4*>(lds + (f ^ (4 * NG * c)) + row0 * L::P);
   }
   __device__ __forceinline__ f32x4 tfrag(const float* lds, int e, int c) const {
-    const int col = e * R + r;
-    f32x4 v;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) v[t] = lds[L::at(4 * g + t, col / 4) + (col & 3) + 4 * NG * c * L::P];
-    return v;
+    const float* p = lds + 4 * NG * c * L::P;
+    return f32x4{p[t0 ^ (R * e)], p[t1 ^ (R * e)], p[t2 ^ (R * e)], p[t3 ^ (R * e)]};
   }
 };
 
@@ -1034,7 +1040,7 @@ struct Shape {
   static constexpr int KB = BIG && (DUAL ? F32 || PASS != DKV : !F32 && PASS == FWD) ? 32 : 64;
   static constexpr int SB = KB == 32 && KS == 2 ? 16 : 32;
   static constexpr int MW = F32 || (DUAL && BIG && PASS == DKV) ? 1 : 2;
-  static constexpr bool PIN = !F32 && BIG && (DUAL ? PASS != FWD : PASS == FWD);
+  static constexpr bool PIN = F32 ? BIG && DUAL : BIG ? (DUAL ? PASS != FWD : PASS == FWD) : DUAL && SMALL;
   static constexpr int KIND = tile_kind(NW * R / KS);
 };
 
