@@ -334,6 +334,8 @@ mfmg_status mfmg_meta_grad_noalloc(mfmg_problem_t problem, const float* theta0,
  * Tangents (names ending in d, and xd / dxd structs) are given together or not at
  * all: with them a call also returns the derivative of its outputs along them.
  *
+ * Outputs must not alias inputs or each other.
+ *
  * Tokens of several sequences lie behind one another: a plan made from their offsets
  * (mfmg_seq_plan) says which token belongs to which sequence.  Tokens before the first
  * or behind the last one are unused rows: nothing of them enters a result (they may
@@ -385,8 +387,7 @@ void mfmg_attn_destroy(mfmg_attn_t attn);
 /* Workspace bytes of mfmg_qk_rope_bwd and mfmg_attn_bwd for n_tokens rows. */
 mfmg_status mfmg_attn_ws_bytes(mfmg_attn_t attn, int64_t n_tokens, size_t* bytes);
 
-/* Device bytes of a plan over n_tokens rows (< 2^31 - 1024) and n_seqs sequences
- * (<= 2^24). */
+/* Device bytes of a plan over n_tokens rows (< 2^26) and n_seqs sequences (<= 2^20). */
 mfmg_status mfmg_seq_plan_bytes(int64_t n_tokens, int n_seqs, size_t* bytes);
 
 /* Writes the plan of a batch into `plan` (dev, 256-byte aligned).  cu_seqlens (dev,
@@ -402,7 +403,7 @@ mfmg_status mfmg_seq_plan(const int32_t* cu_seqlens, int n_seqs, int64_t n_token
  * qk_norm; value heads are converted to T only.
  *   x, xd (dev, float32 [n_tokens][ldx]), gain, gaind (dev, float32 [2][head_dim]: the
  *   query heads' gain, then the key heads'; required with qk_norm, else NULL),
- *   y, yd (dev, T [n_tokens][ldy]).  Outputs must not alias inputs. */
+ *   y, yd (dev, T [n_tokens][ldy]). */
 mfmg_status mfmg_qk_rope_fwd(mfmg_attn_t attn, const void* plan, int64_t n_tokens, int n_seqs,
                              const float* x, const float* xd, int64_t ldx, const float* gain,
                              const float* gaind, void* y, void* yd, int64_t ldy, void* stream);
@@ -417,7 +418,8 @@ mfmg_status mfmg_qk_rope_bwd(mfmg_attn_t attn, const void* plan, int64_t n_token
                              void* dx, void* dxd, int64_t lddx, float* dgain, float* dgaind,
                              void* ws, size_t ws_bytes, void* stream);
 
-/* Causal softmax attention of every sequence, o (dev, T [n_tokens][ldo]) and, with the
+/* Causal softmax attention of every sequence (heads * n_tokens below 2^30, less for very
+ * many short sequences, else UNSUPPORTED): o (dev, T [n_tokens][ldo]) and, with the
  * tangents xd, od.  stats (dev, float32 [2][heads][n_tokens]): what the backward needs
  * of every row (4-byte aligned). */
 mfmg_status mfmg_attn_fwd(mfmg_attn_t attn, const void* plan, int64_t n_tokens, int n_seqs,

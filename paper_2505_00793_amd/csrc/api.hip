@@ -925,9 +925,9 @@ namespace {
 
 mfmg_status check_tokens(int64_t n, int m) {
   if (n < 0 || n > PK_MAX_TOKENS)
-    return fail(MFMG_ERR_INVALID_ARGUMENT, "n_tokens %lld outside [0, 2^31 - 1024]", (long long)n);
+    return fail(MFMG_ERR_INVALID_ARGUMENT, "n_tokens %lld outside [0, 2^26)", (long long)n);
   if (m < 0 || m > PK_MAX_SEQS)
-    return fail(MFMG_ERR_INVALID_ARGUMENT, "n_seqs %d outside [0, 2^24]", m);
+    return fail(MFMG_ERR_INVALID_ARGUMENT, "n_seqs %d outside [0, 2^20]", m);
   return MFMG_OK;
 }
 
@@ -1592,6 +1592,9 @@ mfmg_status mfmg_attn_fwd(mfmg_attn_t a, const void* plan, int64_t n, int m, con
   if (!x) return fail(MFMG_ERR_INVALID_ARGUMENT, "null x");
   if (!xd != !od) return fail(MFMG_ERR_INVALID_ARGUMENT, "the tangents xd and od go together");
   if (n == 0) return MFMG_OK;
+  if (!attn_grid_fits(n, m, a->d.heads))
+    return fail(MFMG_ERR_UNSUPPORTED, "%lld tokens in %d sequences of %d heads: more than 2^32 threads",
+                (long long)n, m, a->d.heads);
   const int64_t qw = (int64_t)a->d.heads * a->d.head_dim;
   TRY(check_qkv(a, "x", x->q, x->k, x->v, x->ldq, x->ldk, x->ldv));
   TRY(check_rows("o", o, ldo, qw, a->size()));
@@ -1617,6 +1620,9 @@ mfmg_status mfmg_attn_bwd(mfmg_attn_t a, const void* plan, int64_t n, int m, con
   if (dual && !(xd && od && gd && dxd))
     return fail(MFMG_ERR_INVALID_ARGUMENT, "the tangents xd, od, gd and dxd go together");
   if (n == 0) return MFMG_OK;
+  if (!attn_grid_fits(n, m, a->d.heads))
+    return fail(MFMG_ERR_UNSUPPORTED, "%lld tokens in %d sequences of %d heads: more than 2^32 threads",
+                (long long)n, m, a->d.heads);
   const int64_t qw = (int64_t)a->d.heads * a->d.head_dim;
   TRY(check_qkv(a, "x", x->q, x->k, x->v, x->ldq, x->ldk, x->ldv));
   TRY(check_qkv(a, "dx", dx->q, dx->k, dx->v, dx->ldq, dx->ldk, dx->ldv));

@@ -12,8 +12,9 @@ __host__ __device__ constexpr int tile_rows(int kind) { return 32 << kind; }
 __host__ __device__ constexpr int tile_kind(int rows) { return rows == 128 ? 2 : rows == 64 ? 1 : 0; }
 constexpr int PLAN_FIRST = TILE_KINDS, PLAN_LAST = TILE_KINDS + 1;   // of SeqPlan::head
 constexpr int PK_MAX_DH = 128;      // largest head dimension
-constexpr long PK_MAX_TOKENS = (1L << 31) - 1024;
-constexpr int PK_MAX_SEQS = 1 << 24;
+// A grid is at most 2^32 threads: 64 a token for the rotation, and what attn_grid_fits says.
+constexpr long PK_MAX_TOKENS = (1L << 26) - 1;
+constexpr int PK_MAX_SEQS = 1 << 20;
 constexpr int PK_MAX_HEADS = 1024;
 constexpr int ROPE_MAX_PAIRS = PK_MAX_DH / 2;
 
@@ -33,6 +34,11 @@ struct SeqPlan {
   long n;
   int m, max_tiles[TILE_KINDS];
 };
+// Whether the attention grids of `heads` heads over n tokens and m sequences can be launched
+// (256 threads a tile of 64 rows, 512 one of 128).
+inline bool attn_grid_fits(long n, int m, int heads) {
+  return (n / 64 + 2 * (m < n ? (long)m : n) + 1) * heads * 256 < (1L << 32);
+}
 // Layout of a plan over n tokens and m sequences at `base` (null: measure);
 // *bytes receives its size.
 SeqPlan seq_plan_at(char* base, long n, int m, size_t* bytes);

@@ -299,6 +299,7 @@ template <typename T, int DH, int R, int NW, int KS, int KB, int SB, int MW, boo
 __global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<T> a) {
   constexpr int NT = 64 * NW, NG = 64 / R, NS = SB / R, NE = DH / R, FE = FragT<T>::FE, NC = DH / (FE * NG);
   constexpr int AV = R * R / 64, NK = SB / (FE * NG), ROWS = NW * R / KS;
+  static_assert(SB % R == 0, "a wave that takes a sub-block sees its first row");
   typedef typename AccT<R>::V V;
   typedef typename FragT<T>::V F;
   typedef Tile<T, DH> L;

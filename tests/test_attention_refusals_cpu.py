@@ -54,7 +54,7 @@ def test_plan_refusals():
     n = ctypes.c_size_t(0)
     assert _status("mfmg_seq_plan_bytes", 100, 3, ctypes.byref(n)) == M.OK
     need = n.value
-    for bad in ((-1, 3), (1 << 31, 3), (100, -1), (100, (1 << 24) + 1)):
+    for bad in ((-1, 3), (1 << 31, 3), (1 << 26, 3), (100, -1), (100, (1 << 20) + 1)):
         assert _status("mfmg_seq_plan_bytes", *bad, ctypes.byref(n)) == M.ERR_INVALID_ARGUMENT
     call = lambda cu=A, m=3, n=100, pos=None, plan=B, size=need: _status("mfmg_seq_plan", cu, m, n, pos, plan, size, None)
     assert call(cu=None) == M.ERR_INVALID_ARGUMENT
@@ -120,6 +120,9 @@ def test_attention_refusals():
     for kw in bad:
         assert b(**kw) == M.ERR_INVALID_ARGUMENT, kw
     assert b(ws_bytes=need - 1) == M.ERR_WORKSPACE
+    wide = M.Attention(M.make_attn_desc(heads=1024, head_dim=64))   # 2^30 rows of heads
+    x = _qkv(ldq=65536, ldk=65536, ldv=65536)
+    assert _status("mfmg_attn_fwd", wide._h, *{**fwd, "n": 1 << 20, "x": x, "ldo": 65536}.values()) == M.ERR_UNSUPPORTED
     assert _status("mfmg_attn_fwd", None, *fwd.values()) == M.ERR_INVALID_ARGUMENT
 
 

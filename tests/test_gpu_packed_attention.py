@@ -236,3 +236,63 @@ def test_many_rows_against_float64(prec, dual, H, K, dh, lens):
     c = Call(prec, H, K, dh, lens, dual, before=1, after=9, gap=16).run()
     torch.cuda.synchronize()
     c.check()
+
+
+def test_offsets_are_clamped_and_made_ascending():
+    """Offsets past the rows, negative or descending: the same plan as their running maximum within the
+    rows, more sequences than tokens and than one pass of the planning among them."""
+    M = _lib()
+    print("\n[packed] wild offsets", flush=True)
+    n, H, dh = 700, 2, 32
+    g = torch.Generator().manual_seed(2)
+    wild = torch.randint(-200, 900, (3000,), generator=g, dtype=torch.int32)
+    wild[0] = 5
+    wild[1:2000] = wild[1:2000].clamp(max=300)
+    wild[2990] = 2 ** 31 - 1
+    wild[2995] = -2 ** 31
+    tame = wild.clamp(0, n).cummax(0).values.to(torch.int32)
+    op = M.Attention(M.make_attn_desc(heads=H, kv_heads=1, head_dim=dh))
+    x = torch.randn(n, (H + 2) * dh, device="cuda", generator=torch.Generator(device="cuda").manual_seed(3))
+    cut = (H * dh, dh, dh)
+    res = []
+    for cu in (wild, tame, tame.unique_consecutive()):
+        plan = M.mfmg_seq_plan(cu.cuda(), n)
+        o, dx = torch.full((n, H * dh), 7.0, device="cuda"), torch.full_like(x, 7.0)
+        y = torch.full_like(x, 7.0)
+        stats = torch.empty(2, H, n, device="cuda")
+        op.mfmg_qk_rope_fwd(plan, x, y)
+        op.mfmg_attn_fwd(plan, *x.split(cut, 1), o, stats)
+        op.mfmg_attn_bwd(plan, *x.split(cut, 1), o, stats, x[:, :H * dh], *dx.split(cut, 1))
+        torch.cuda.synchronize()
+        res.append((o, dx, y))
+    for got in res[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(got, res[0]))
+    first = int(tame[0])
+    assert torch.equal(res[0][0][:first], torch.full((first, H * dh), 7.0, device="cuda"))
+
+
+def test_many_tiles_of_one_length_class():
+    """More tiles than the planning's classes of length, one long sequence among short ones: every tile
+    is done once."""
+    M = _lib()
+    print("\n[packed] many tiles", flush=True)
+    lens = [40000] + [3, 65, 1, 130] * 700
+    n = sum(lens)
+    op = M.Attention(M.make_attn_desc(heads=1, head_dim=8, precision=1))
+    cu = torch.tensor([0] + lens).cumsum(0).to(torch.int32).cuda()
+    plan = M.mfmg_seq_plan(cu, n)
+    v = torch.ones(n, 8, device="cuda", dtype=torch.bfloat16)
+    q, k = (torch.randn(n, 8, device="cuda").bfloat16() for _ in range(2))
+    o, dv = torch.zeros_like(v), torch.zeros_like(v)
+    dq, dk = torch.ones_like(v), torch.ones_like(v)
+    stats = torch.empty(2, 1, n, device="cuda")
+    op.mfmg_attn_fwd(plan, q, k, v, o, stats)
+    assert (o.float() - 1).abs().max() <= 2 ** -6   # weights of a row sum to 1: P's rounding and o's
+    op.mfmg_attn_bwd(plan, q, k, v, o, stats, v, dq, dk, dv)
+    torch.cuda.synchronize()
+    # the columns' weights sum to the number of rows; v is constant, so dP is, and dS vanishes
+    per = dv.float()[:, 0].double().cpu()
+    ends = cu.cpu().tolist()
+    for a, b in zip(ends, ends[1:]):
+        assert abs(float(per[a:b].sum()) / (b - a) - 1) <= 2 ** -7
+    assert dq.float().abs().max() < 1 and dk.float().abs().max() < 1
