@@ -150,9 +150,9 @@ def _batch(x, y):
     return mfmg_batch(x.data_ptr(), None if y is None else y.data_ptr(), x.shape[0])
 
 
-def _stream(device=None):
+def _stream():
     import torch
-    return torch.cuda.current_stream(device).cuda_stream
+    return torch.cuda.current_stream().cuda_stream
 
 
 def make_desc(*, widths, act=0, loss=1, optimizer=0, meta=0, precision=0, has_bias=True, rows=1,
@@ -280,6 +280,13 @@ def _device() -> int:
     return torch.cuda.current_device() if torch.cuda.is_initialized() else 0
 
 
+def _raw_stream(device: int) -> int:
+    """The current stream's handle, without a stream object where torch offers it."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device) if raw else torch.cuda.current_stream(device).cuda_stream
+
+
 class SeqPlan:
     """The plan of a batch's sequences (mfmg_seq_plan): device memory with its sizes."""
 
@@ -400,7 +407,7 @@ class Attention:
         ldy = self._pair("y", y, yd, w, self.dtype, n, dev)
         self._gains(dev, gain, gaind)
         check(lib().mfmg_qk_rope_fwd(*self._head(plan, dev), _addr(x), _addr(xd), ldx, _addr(gain),
-                                     _addr(gaind), _addr(y), _addr(yd), ldy, _stream(dev)))
+                                     _addr(gaind), _addr(y), _addr(yd), ldy, _raw_stream(dev)))
 
     def mfmg_qk_rope_bwd(self, plan, dy, dx, x=None, gain=None, dgain=None, dyd=None, dxd=None,
                          xd=None, gaind=None, dgaind=None, ws=None):
@@ -413,7 +420,7 @@ class Attention:
             ws = self.workspace(n, dy.device)
         check(lib().mfmg_qk_rope_bwd(*self._head(plan, dev, ws), _addr(x), _addr(xd), ldx, _addr(gain),
                                      _addr(gaind), _addr(dy), _addr(dyd), lddy, _addr(dx), _addr(dxd),
-                                     lddx, _addr(dgain), _addr(dgaind), _addr(ws), ws.numel(), _stream(dev)))
+                                     lddx, _addr(dgain), _addr(dgaind), _addr(ws), ws.numel(), _raw_stream(dev)))
 
     def _stats(self, stats, n, device):
         _check_dev("stats", stats, self.float32, device)
@@ -426,7 +433,7 @@ class Attention:
         ldo = self._pair("o", o, od, self.q_cols, self.dtype, n, dev)
         check(lib().mfmg_attn_fwd(*self._head(plan, dev), self._qkv("x", q, k, v, n, dev),
                                   self._qkv("xd", qd, kd, vd, n, dev), _addr(o), _addr(od), ldo,
-                                  self._stats(stats, n, dev), _stream(dev)))
+                                  self._stats(stats, n, dev), _raw_stream(dev)))
 
     def mfmg_attn_bwd(self, plan, q, k, v, o, stats, g, dq, dk, dv, qd=None, kd=None, vd=None,
                       od=None, dod=None, dqd=None, dkd=None, dvd=None, ws=None):
@@ -440,7 +447,7 @@ class Attention:
                                   self._stats(stats, n, dev), _addr(g), _addr(dod), ldg,
                                   self._qkv("dx", dq, dk, dv, n, dev),
                                   self._qkv("dxd", dqd, dkd, dvd, n, dev), _addr(ws), ws.numel(),
-                                  _stream(dev)))
+                                  _raw_stream(dev)))
 
 
 def mfmg_check_finite(x, ws=None) -> int:
