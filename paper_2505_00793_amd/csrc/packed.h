@@ -6,10 +6,12 @@
 
 namespace mfmg {
 
-// Attention tiles of three sizes: 32, 64 and 128 rows (queries or keys).
-constexpr int TILE_KINDS = 3;
-__host__ __device__ constexpr int tile_rows(int kind) { return 32 << kind; }
-__host__ __device__ constexpr int tile_kind(int rows) { return rows == 128 ? 2 : rows == 64 ? 1 : 0; }
+// Attention tiles of four sizes: 16, 32, 64 and 128 rows (queries or keys).
+constexpr int TILE_KINDS = 4;
+__host__ __device__ constexpr int tile_rows(int kind) { return 16 << kind; }
+__host__ __device__ constexpr int tile_kind(int rows) {
+  return rows == 128 ? 3 : rows == 64 ? 2 : rows == 32 ? 1 : 0;
+}
 constexpr int PLAN_FIRST = TILE_KINDS, PLAN_LAST = TILE_KINDS + 1;   // of SeqPlan::head
 constexpr int PK_MAX_DH = 128;      // largest head dimension
 // A grid is at most 2^32 threads: 64 a token for the rotation, and what attn_grid_fits says.

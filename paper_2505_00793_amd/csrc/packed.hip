@@ -250,26 +250,27 @@ __device__ __forceinline__ void store_row(T* row, const V (&acc)[NE], float f, i
   }
 }
 
-// Two waves that own the same rows and every other SB of the other side (KS = 2) join
-// their sums in LDS, lane by lane: the odd wave's times f1 are added to the even wave's
-// times f0.  All waves call this together; `lds` is free for it.
+// KS waves that own the same rows and every KS-th sub-block of the other side join their
+// sums in LDS, lane by lane and in order, in the first of them.  All waves call this
+// together; `lds` is free for it.
 template <int R, int NE, int KS>
 struct Merge {
   static constexpr int AV = R * R / 64, LANE = NE * AV + 3;   // floats of a lane: an array, 3 scalars
   float* p;
-  bool odd;
+  int rank;   // 0 .. KS - 1
   __device__ __forceinline__ Merge(float* lds, int w, int lane)
-      : p(lds + w / KS * LANE * 64 + lane), odd(w % KS) {}
+      : p(lds + w / KS * LANE * 64 + lane), rank(w % KS) {}
   __device__ __forceinline__ float& scalar(int i) { return p[(NE * AV + i) * 64]; }
+  // from wave j: v of the first wave becomes v f0 + v_j f1
   template <typename V>
-  __device__ __forceinline__ void add(V (&v)[NE], float f0, float f1) {
+  __device__ __forceinline__ void add(int j, V (&v)[NE], float f0, float f1) {
     __syncthreads();
-    if (odd) {
+    if (rank == j) {
 #pragma unroll
       for (int t = 0; t < NE * AV; ++t) p[t * 64] = v[t / AV][t % AV];
     }
     __syncthreads();
-    if (!odd) {
+    if (rank == 0) {
 #pragma unroll
       for (int t = 0; t < NE * AV; ++t) v[t / AV][t % AV] = v[t / AV][t % AV] * f0 + p[t * 64] * f1;
     }
@@ -443,28 +444,31 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<
     if (kb + 1 < nb) block(kb + 1, std::integral_constant<int, 1>());
   }
   if constexpr (KS > 1) {
-    // the other half of the keys joins in, both at the larger maximum
+    // the other waves' keys join in, at the larger maximum
     Merge<R, NE, KS> M(reinterpret_cast<float*>(&sK[0][0]), w, lane);
     static_assert(NW / KS * M.LANE * 256 <= sizeof(sK), "merge buffer");
-    __syncthreads();
-    if (M.odd) {
-      M.scalar(0) = m;
-      M.scalar(1) = l;
-      M.scalar(2) = cs;
+#pragma unroll
+    for (int j = 1; j < KS; ++j) {
+      __syncthreads();
+      if (M.rank == j) {
+        M.scalar(0) = m;
+        M.scalar(1) = l;
+        M.scalar(2) = cs;
+      }
+      __syncthreads();
+      float f0 = 1.f, f1 = 1.f;
+      if (M.rank == 0) {   // (the first wave has seen the first key: its maximum is finite)
+        const float m1 = M.scalar(0), mn = fmaxf(m, m1);
+        f0 = exp2_(m - mn);
+        f1 = exp2_(m1 - mn);
+        m = mn;
+        l = l * f0 + M.scalar(1) * f1;
+        cs = cs * f0 + M.scalar(2) * f1;
+      }
+      M.add(j, o, f0, f1);
+      if constexpr (DUAL) M.add(j, od, f0, f1);
     }
-    __syncthreads();
-    float f0 = 1.f, f1 = 1.f;
-    if (!M.odd) {   // (the even wave has seen the first key: its maximum is finite)
-      const float m1 = M.scalar(0), mn = fmaxf(m, m1);
-      f0 = exp2_(m - mn);
-      f1 = exp2_(m1 - mn);
-      m = mn;
-      l = l * f0 + M.scalar(1) * f1;
-      cs = cs * f0 + M.scalar(2) * f1;
-    }
-    M.add(o, f0, f1);
-    if constexpr (DUAL) M.add(od, f0, f1);
-    if (M.odd) return;
+    if (M.rank) return;
   }
   if (q >= hi) return;   // (lanes of one row leave together; q0 < hi has l > 0)
   const float lt = sum_groups<R>(l), inv = 1.0f / lt;
@@ -644,9 +648,12 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T
   if constexpr (KS > 1) {
     Merge<R, NE, KS> M(reinterpret_cast<float*>(&sK[0][0]), w, lane);
     static_assert(NW / KS * M.LANE * 256 <= sizeof(sK), "merge buffer");
-    M.add(dq, 1.f, 1.f);
-    if constexpr (DUAL) M.add(dqd, 1.f, 1.f);
-    if (M.odd) return;
+#pragma unroll
+    for (int j = 1; j < KS; ++j) {
+      M.add(j, dq, 1.f, 1.f);
+      if constexpr (DUAL) M.add(j, dqd, 1.f, 1.f);
+    }
+    if (M.rank) return;
   }
   if (q >= hi) return;
   store_row<R, NE>(a.dq + q * a.lddq + (long)h * dh, dq, a.scale, g, dh);
@@ -839,13 +846,16 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dkv_kernel(PackedAttnArgs<
   if constexpr (KS > 1) {
     Merge<R, NE, KS> M(reinterpret_cast<float*>(&sQ[0][0]), w, lane);
     static_assert(NW / KS * M.LANE * 256 <= sizeof(sQ), "merge buffer");
-    M.add(dk, 1.f, 1.f);
-    M.add(dv, 1.f, 1.f);
-    if constexpr (DUAL) {
-      M.add(dkd, 1.f, 1.f);
-      M.add(dvd, 1.f, 1.f);
+#pragma unroll
+    for (int j = 1; j < KS; ++j) {
+      M.add(j, dk, 1.f, 1.f);
+      M.add(j, dv, 1.f, 1.f);
+      if constexpr (DUAL) {
+        M.add(j, dkd, 1.f, 1.f);
+        M.add(j, dvd, 1.f, 1.f);
+      }
     }
-    if (M.odd) return;
+    if (M.rank) return;
   }
   if (k >= hi) return;
   if (a.parts > 1) {
@@ -1032,26 +1042,26 @@ int dkv_parts(long n, int H, int K) {
 //   11.4, 15.4; float32: 1531 tokens of 6 heads, pairs of waves sharing 32 rows 62, 79, 105,
 //   64-row tiles 118, 166, 229).
 enum Pass { FWD, DQ, DKV };
-template <typename T, int DH, bool DUAL, int PASS, bool SMALL>
+template <typename T, int DH, bool DUAL, int PASS, int SMALL>
 struct Shape {
   static constexpr bool F32 = sizeof(T) == 4, BIG = DH > 64;
   static constexpr int R = !F32 && !DUAL && PASS != DKV && !SMALL ? 32 : 16;
   static constexpr int NW = !F32 && DUAL && !BIG && !SMALL ? 8 : 4;
-  static constexpr int KS = F32 && SMALL ? 2 : 1;
+  static constexpr int KS = F32 && SMALL ? 2 * SMALL : 1;
   static constexpr int KB = BIG && (DUAL ? F32 || PASS != DKV : !F32 && PASS == FWD) ? 32 : 64;
-  static constexpr int SB = KB == 32 && KS == 2 ? 16 : 32;
+  static constexpr int SB = F32 && KB < 32 * KS ? 16 : 32;
   static constexpr int MW = F32 || (DUAL && BIG && PASS == DKV) ? 1 : 2;
   static constexpr bool PIN = F32 ? BIG && DUAL : BIG ? (DUAL ? PASS != FWD : PASS == FWD) : DUAL && SMALL;
   static constexpr int KIND = tile_kind(NW * R / KS);
 };
 
-template <typename T, int DH, bool DUAL, bool SMALL>
+template <typename T, int DH, bool DUAL, int SMALL>
 void launch_fwd(const PackedAttnArgs<T>& a, hipStream_t s) {
   typedef Shape<T, DH, DUAL, FWD, SMALL> S;
   hipLaunchKernelGGL((packed_fwd_kernel<T, DH, S::R, S::NW, S::KS, S::KB, S::SB, S::MW, S::PIN, DUAL>),
                      dim3(a.p.max_tiles[S::KIND] * a.H), dim3(64 * S::NW), 0, s, a);
 }
-template <typename T, int DH, bool DUAL, bool SMALL>
+template <typename T, int DH, bool DUAL, int SMALL>
 hipError_t launch_bwd(const PackedAttnArgs<T>& a, hipStream_t s) {
   typedef Shape<T, DH, DUAL, DQ, SMALL> Q;
   typedef Shape<T, DH, DUAL, DKV, SMALL> S;
@@ -1068,23 +1078,35 @@ hipError_t launch_bwd(const PackedAttnArgs<T>& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Few rows: smaller tiles, so that more workgroups share the work.
-template <typename T>
-bool small(const PackedAttnArgs<T>& a) {
-  return a.p.n * a.H < (sizeof(T) == 4 ? 512 * 64 : 512 * 128);
+// Few rows: smaller tiles, so that more workgroups share the work.  2, float32 only: four
+// waves a 16-row tile, where sequences are long enough to divide (primal 1500 tokens of 8
+// heads in 3 sequences 141 -> 110 us, dual 1531 of 6 in 4 257 -> 208; but dual 2000 of 8
+// in 3 432 -> 484, 200 of 8 in 30 43 -> 60) and a staged block holds four sub-blocks.
+template <typename T, int DH>
+int small(const PackedAttnArgs<T>& a) {
+  const long rows = a.p.n * a.H;
+  if (sizeof(T) == 2) return rows < 512 * 128;
+  if (rows < 192 * 64 && a.p.n >= 256L * a.p.m && !(DH > 64 && a.dual)) return 2;
+  return rows < 512 * 64;
+}
+template <typename T, int DH, int SMALL>
+hipError_t run_at(const PackedAttnArgs<T>& a, bool bwd, hipStream_t s) {
+  if (bwd) return a.dual ? launch_bwd<T, DH, true, SMALL>(a, s) : launch_bwd<T, DH, false, SMALL>(a, s);
+  if (a.dual) launch_fwd<T, DH, true, SMALL>(a, s); else launch_fwd<T, DH, false, SMALL>(a, s);
+  return hipGetLastError();
 }
 template <typename T, int DH>
 hipError_t run(const PackedAttnArgs<T>& a, bool bwd, hipStream_t s) {
-  if (bwd) {
-    if (small(a)) return a.dual ? launch_bwd<T, DH, true, true>(a, s) : launch_bwd<T, DH, false, true>(a, s);
-    return a.dual ? launch_bwd<T, DH, true, false>(a, s) : launch_bwd<T, DH, false, false>(a, s);
+  const int level = small<T, DH>(a);
+  if constexpr (sizeof(T) == 4) {
+    if (level == 2) {
+      if constexpr (DH <= 64) return run_at<T, DH, 2>(a, bwd, s);
+      if (bwd) return launch_bwd<T, DH, false, 2>(a, s);   // (primal: see small)
+      launch_fwd<T, DH, false, 2>(a, s);
+      return hipGetLastError();
+    }
   }
-  if (small(a)) {
-    if (a.dual) launch_fwd<T, DH, true, true>(a, s); else launch_fwd<T, DH, false, true>(a, s);
-  } else {
-    if (a.dual) launch_fwd<T, DH, true, false>(a, s); else launch_fwd<T, DH, false, false>(a, s);
-  }
-  return hipGetLastError();
+  return level ? run_at<T, DH, 1>(a, bwd, s) : run_at<T, DH, 0>(a, bwd, s);
 }
 // The products' head dimension: dh rounded up to one that is compiled (columns past dh are
 // zero in one operand, or not stored).

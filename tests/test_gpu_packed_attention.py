@@ -296,3 +296,14 @@ def test_many_tiles_of_one_length_class():
     for a, b in zip(ends, ends[1:]):
         assert abs(float(per[a:b].sum()) / (b - a) - 1) <= 2 ** -7
     assert dq.float().abs().max() < 1 and dk.float().abs().max() < 1
+
+
+@pytest.mark.parametrize("dual", [False, True], ids=["primal", "dual"])
+@pytest.mark.parametrize("H,K,dh,lens", [(2, 1, 64, [900, 333]), (4, 2, 40, [515]), (3, 3, 128, [600, 20, 270]),
+                                         (1, 1, 24, [256])], ids=lambda v: str(v).replace(" ", ""))
+def test_few_long_float32_rows(dual, H, K, dh, lens):
+    """Float32 rows few enough for tiles whose four waves share them."""
+    print(f"\n[packed] H {H} K {K} dh {dh} lens {lens} dual {dual}", flush=True)
+    c = Call(0, H, K, dh, lens, dual, before=0, after=2).run()
+    torch.cuda.synchronize()
+    c.check()
