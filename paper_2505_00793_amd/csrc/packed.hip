@@ -22,12 +22,20 @@
 //
 // Fragments.  A wave owns R = 16 or 32 rows (queries, or keys in the dK/dV pass) and
 // lane l = R g + i holds row i; NG = 64 / R lane groups g.  Products are formed as
-// C[a][b] = sum_k A[a][k] B[b][k] with b the lane's row: an operand fragment is the 8
-// elements k = 8 g + 0..7 of 8 NG, and of R x R results the lane holds a =
-// 4 NG (t / 4) + 4 g + t % 4 of its row.  So the scores of a 64-row block leave a lane
-// with the values at 64-block rows idx(t) = 4 NG (t / 4) + 4 g + t % 4, eight of which
-// are a fragment of the next product, over rows in that order; its other operand is
-// read from the tile in the same order (tfrag), and probabilities never leave registers.
+// C[a][b] = sum_k A[a][k] B[b][k] with b the lane's row: an operand fragment is the FE
+// elements k = FE g + 0 .. FE - 1 of FE NG (FE = 8 for bf16, 4 for float32), and of R x R
+// results the lane holds a = idx(t) = 4 NG (t / 4) + 4 g + t % 4 of its row.  So the
+// scores of a block leave a lane with the values at block rows idx(t), FE of which are a
+// fragment of the next product, over rows in that order; its other operand is read from
+// the tile in the same order (tfrag), and probabilities never leave registers.
+//
+// What bounds it.  The matrix instructions: 2 and 6 products a visible pair in the primal
+// and dual forward, 3 and 9 in the dQ pass, 4 and 12 in the dK/dV pass, where S and dP
+// are formed again so that no sum needs atomics (a single pass would take 5 and 15 for
+// the backward, not 7 and 21).  They are fed from LDS, one fragment read a product and R
+// rows, by two or three waves a SIMD, whose exponentials run beside another's products.
+// Counters at 16384 tokens of 16 heads of 128: matrix units busy 45% of the cycles at the
+// 2.0 GHz the card then holds, vector units 38%, no bank conflicts.
 #include "packed.h"
 
 #include <algorithm>
@@ -290,7 +298,9 @@ __device__ __forceinline__ void tile_of(int heads, int& rank, int& head) {
 }
 
 // ---------------------------------------------------------------- forward
-// A workgroup owns NW R queries of one head.  Scores are formed for SB keys at a time
+// 16384 tokens of 16 heads of 128 over 2 key heads, bf16: 1.15 ms, 0.96 PFLOP/s (a bf16
+// product of 8192^3 reaches 1.21); dual, 2 x 4096 tokens of 8 heads of 64: 122 us, 0.84.
+// A workgroup owns NW R / KS queries of one head.  Scores are formed for SB keys at a time
 // and consumed before the next SB, which bounds the registers they need.  The running
 // maximum is only raised, and the accumulators rescaled, when a score exceeds it by
 // more than 2^8: until then exp2 stays below 2^8 times its usual range, far from
@@ -496,7 +506,9 @@ __device__ __forceinline__ float dot(const f32x4& a, const f32x4& b) {
   return a[0] * b[0] + a[1] * b[1] + a[2] * b[2] + a[3] * b[3];
 }
 
-// Scores' cotangents are formed without the scale s, which the sums take at the end.
+// 40 sequences of 16001 tokens, 16 heads of 128 over 2: 165 us, 0.56 PFLOP/s; dual, 2 x 4096
+// tokens of 8 heads of 64: 157 us, 0.98.  Score cotangents are formed without the scale s,
+// which the sums take at the end.
 template <typename T, int DH, int R, int NW, int KS, int KB, int SB, int MW, bool PIN, bool DUAL>
 __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T> a) {
   constexpr int NT = 64 * NW, NG = 64 / R, NS = SB / R, NE = DH / R, FE = FragT<T>::FE, NC = DH / (FE * NG);
@@ -661,7 +673,8 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T
 }
 
 // ---------------------------------------------------------------- backward: dK, dV
-// A workgroup owns NW R keys of one key head and goes through the queries of some of the
+// The same calls: 209 us and 23 to add the parts, 0.54 PFLOP/s; dual 214 us, 0.96.
+// A workgroup owns NW R / KS keys of one key head and goes through the queries of some of the
 // head's query heads (all, or one part of `parts`, whose float32 sums dkv_sum_kernel
 // adds in order).
 template <typename T, int DH, int R, int NW, int KS, int KB, int SB, int MW, bool PIN, bool DUAL>
@@ -897,52 +910,56 @@ __global__ void __launch_bounds__(256) dkv_sum_kernel(PackedAttnArgs<T> a) {
 // ---------------------------------------------------------------- plan
 // Bounds made ascending (running maximum of the clamped offsets) and, for every tile
 // size, the tiles before each sequence, by one workgroup over chunks of its size.
-constexpr int SCAN = 1024;
+constexpr int SCAN = 1024, SCAN_WAVES = SCAN / 64;
+
+// Inclusive scan over the workgroup (and the total): in waves by shuffles, then over the
+// waves' totals in `lds`.
+template <typename Op>
+__device__ __forceinline__ int scan(int v, Op op, int* lds, int& total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int x = __shfl_up(v, o, 64);
+    if (lane >= o) v = op(v, x);
+  }
+  __syncthreads();   // (lds may still be read by the last scan)
+  if (lane == 63) lds[w] = v;
+  __syncthreads();
+  total = lds[0];
+#pragma unroll
+  for (int i = 1; i < SCAN_WAVES; ++i) {
+    if (w == i) v = op(v, total);
+    total = op(total, lds[i]);
+  }
+  return v;
+}
+
 __global__ void __launch_bounds__(SCAN) plan_scan_kernel(SeqPlanArgs a) {
-  __shared__ int sv[SCAN], carry;
+  __shared__ int lds[SCAN_WAVES];
   const int tid = threadIdx.x, m = a.p.m, n = (int)a.p.n;
   auto raw = [&](int j) {
     if (!a.cu) return (int)min((long)j * a.len, (long)n);
     if (!a.cover) return min(max(a.cu[j], 0), n);
     return j == 0 ? 0 : j == m ? n : min(max(a.cu[j - 1], 0), n);
   };
-  if (tid == 0) carry = 0;
+  int carry = 0, total;
   for (int j0 = 0; j0 <= m; j0 += SCAN) {
     const int j = j0 + tid;
-    __syncthreads();
-    sv[tid] = j <= m ? raw(j) : 0;
-    for (int o = 1; o < SCAN; o <<= 1) {
-      __syncthreads();
-      const int x = tid >= o ? sv[tid - o] : 0;
-      __syncthreads();
-      sv[tid] = max(sv[tid], x);
-    }
-    __syncthreads();
-    if (j <= m) a.p.bound[j] = max(sv[tid], carry);
-    __syncthreads();
-    if (tid == 0) carry = max(carry, sv[SCAN - 1]);
+    const int v = scan(j <= m ? raw(j) : 0, [](int x, int y) { return max(x, y); }, lds, total);
+    if (j <= m) a.p.bound[j] = max(v, carry);
+    carry = max(carry, total);
   }
+  __syncthreads();
   for (int kind = 0; kind < TILE_KINDS; ++kind) {
     const int rows = tile_rows(kind);
-    __syncthreads();
-    if (tid == 0) carry = 0;
+    carry = 0;
     for (int j0 = 0; j0 <= m; j0 += SCAN) {
       const int j = j0 + tid;
-      __syncthreads();
       const int t = j < m ? (a.p.bound[j + 1] - a.p.bound[j] + rows - 1) / rows : 0;
-      sv[tid] = t;
-      for (int o = 1; o < SCAN; o <<= 1) {
-        __syncthreads();
-        const int x = tid >= o ? sv[tid - o] : 0;
-        __syncthreads();
-        sv[tid] += x;
-      }
-      __syncthreads();
-      if (j <= m) a.p.list[kind].tstart[j] = carry + sv[tid] - t;
-      __syncthreads();
-      if (tid == 0) carry += sv[SCAN - 1];
+      const int v = scan(t, [](int x, int y) { return x + y; }, lds, total);
+      if (j <= m) a.p.list[kind].tstart[j] = carry + v - t;
+      carry += total;
     }
-    __syncthreads();
     if (tid == 0) a.p.head[kind] = carry;
   }
   if (tid == 0) {
@@ -979,7 +996,7 @@ __global__ void __launch_bounds__(SCAN) plan_fill_kernel(SeqPlanArgs a) {
     a.p.pos[i] = pos;
     return;
   }
-  __shared__ int count[SCAN], longest;
+  __shared__ int count[SCAN], longest, lds[SCAN_WAVES];
   const int kind = blockIdx.x >> 1, byk = blockIdx.x & 1, rows = tile_rows(kind);
   const TileList l = a.p.list[kind];
   const int nt = a.p.head[kind];
@@ -998,15 +1015,9 @@ __global__ void __launch_bounds__(SCAN) plan_fill_kernel(SeqPlanArgs a) {
   for (int i = tid; i < nt; i += SCAN) atomicAdd(&count[SCAN - 1 - length(i, t) / step], 1);
   __syncthreads();
   const int own = count[tid];
-  for (int o = 1; o < SCAN; o <<= 1) {
-    const int x = tid >= o ? count[tid - o] : 0;
-    __syncthreads();
-    count[tid] += x;
-    __syncthreads();
-  }
-  const int before = count[tid] - own;
-  __syncthreads();
-  count[tid] = before;
+  int total;
+  const int before = scan(own, [](int x, int y) { return x + y; }, lds, total) - own;
+  count[tid] = before;   // (every thread's own class)
   __syncthreads();
   int4* out = byk ? l.byk : l.byq;
   for (int i = tid; i < nt; i += SCAN) {
