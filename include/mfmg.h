@@ -340,7 +340,9 @@ mfmg_status mfmg_meta_grad_noalloc(mfmg_problem_t problem, const float* theta0,
  * (mfmg_seq_plan) says which token belongs to which sequence.  Tokens before the first
  * or behind the last one are unused rows: nothing of them enters a result (they may
  * hold anything) and output rows of theirs stay as they were.  Nothing of one sequence
- * enters another's results either, NaN and infinities included.
+ * enters another's results either, NaN and infinities included.  Within a sequence a
+ * later token enters with weight 0, so one that is not finite may make earlier
+ * tokens' results NaN.
  */
 /* How rotary frequencies theta_j = rope_base^(-2j / rope_dims), j < rope_dims / 2, are
  * stretched for contexts longer than those trained on, by rope_factor f >= 1:

@@ -34,8 +34,8 @@
 // are formed again so that no sum needs atomics (a single pass would take 5 and 15 for
 // the backward, not 7 and 21).  They are fed from LDS, one fragment read a product and R
 // rows, by two or three waves a SIMD, whose exponentials run beside another's products.
-// Counters at 16384 tokens of 16 heads of 128: matrix units busy 45% of the cycles at the
-// 2.0 GHz the card then holds, vector units 38%, no bank conflicts.
+// Counters at 16384 tokens of 16 heads of 128: matrix units busy 48% of the cycles at the
+// 1.93 GHz the card then holds, vector units 49%, no bank conflicts.
 #include "packed.h"
 
 #include <algorithm>
@@ -298,7 +298,7 @@ __device__ __forceinline__ void tile_of(int heads, int& rank, int& head) {
 }
 
 // ---------------------------------------------------------------- forward
-// 16384 tokens of 16 heads of 128 over 2 key heads, bf16: 1.15 ms, 0.96 PFLOP/s (a bf16
+// 16384 tokens of 16 heads of 128 over 2 key heads, bf16: 1.11 ms, 0.99 PFLOP/s (a bf16
 // product of 8192^3 reaches 1.21); dual, 2 x 4096 tokens of 8 heads of 64: 122 us, 0.84.
 // A workgroup owns NW R / KS queries of one head.  Scores are formed for SB keys at a time
 // and consumed before the next SB, which bounds the registers they need.  The running
@@ -506,7 +506,7 @@ __device__ __forceinline__ float dot(const f32x4& a, const f32x4& b) {
   return a[0] * b[0] + a[1] * b[1] + a[2] * b[2] + a[3] * b[3];
 }
 
-// 40 sequences of 16001 tokens, 16 heads of 128 over 2: 165 us, 0.56 PFLOP/s; dual, 2 x 4096
+// 40 sequences of 16001 tokens in all, 16 heads of 128 over 2: 165 us, 0.56 PFLOP/s; dual, 2 x 4096
 // tokens of 8 heads of 64: 157 us, 0.98.  Score cotangents are formed without the scale s,
 // which the sums take at the end.
 template <typename T, int DH, int R, int NW, int KS, int KB, int SB, int MW, bool PIN, bool DUAL>
@@ -908,6 +908,7 @@ __global__ void __launch_bounds__(256) dkv_sum_kernel(PackedAttnArgs<T> a) {
 }
 
 // ---------------------------------------------------------------- plan
+// Once a batch: 6 us for the scan, 5 to 10 for the lists and positions at up to 16384 tokens.
 // Bounds made ascending (running maximum of the clamped offsets) and, for every tile
 // size, the tiles before each sequence, by one workgroup over chunks of its size.
 constexpr int SCAN = 1024, SCAN_WAVES = SCAN / 64;
@@ -1039,7 +1040,7 @@ int dkv_parts(long n, int H, int K) {
 // Rows a wave owns, waves of a workgroup, waves that share rows, rows of a staged block, rows
 // of it that a wave forms and consumes scores of at a time, waves a SIMD holds, addresses
 // pinned (Lane).  What they were chosen by, in us:
-//  forward and dQ, 128 dims, bf16 (16 x 400 tokens of 16 heads | 16384 tokens): 32 rows a
+//  forward and dQ, 128 dims, bf16 (16001 tokens in 40 sequences of 16 heads | 16384 in one): 32 rows a
 //   wave, 4 waves, 104 | 1160 and 170; 16 rows, 4 waves 115 | 1380 and 178 (twice the LDS
 //   reads a product); 16 rows, 8 waves 110 | 1200 and 200;
 //  dK/dV, 128 dims: 16 rows, 4 waves 209; 16 rows, 8 waves 246; 32 rows need more

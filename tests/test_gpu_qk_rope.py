@@ -238,3 +238,29 @@ def test_block_of_operators_matches_autograd_and_differences():
     # times the amplification of a second derivative
     for got, a, b in zip((od, dxd, dgaind), up, dn):
         assert rel(got, (a - b) / (2 * h)) <= 1000 * R.E
+
+
+@pytest.mark.parametrize("dual", [False, True], ids=["primal", "dual"])
+@pytest.mark.parametrize("prec", [0, 1], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("dh,dims,inter", [(64, 16, False), (64, 10, False), (64, 6, True), (8, 2, True), (128, 96, False)])
+def test_infinities_pass_where_nothing_rotates(prec, dual, dh, dims, inter):
+    """An infinity in a dim that does not rotate comes out as it is and reaches no other dim."""
+    from paper_2505_00793_amd import _lib as M
+    T = torch.bfloat16 if prec else torch.float32
+    op = M.Attention(M.make_attn_desc(heads=3, kv_heads=1, head_dim=dh, precision=prec,
+                                      **{**FREE, "rope_dims": dims, "rope_interleaved": inter}))
+    n, W = 9, 5 * dh
+    plan = M.mfmg_seq_plan(torch.tensor([0, n], dtype=torch.int32, device="cuda"), n)
+    x = torch.ones(n, W, device="cuda")
+    at = torch.zeros(n, W, dtype=torch.bool, device="cuda")
+    at.view(n, 5, dh)[:, :, dims:][::2, ::2, ::3] = True
+    x[at] = float("inf")
+    xd = x if dual else None
+    y, dx = (torch.zeros(n, W, device="cuda", dtype=T) for _ in range(2))
+    yd, dxd = (torch.zeros(n, W, device="cuda", dtype=T) if dual else None for _ in range(2))
+    op.mfmg_qk_rope_fwd(plan, x, y, xd=xd, yd=yd)
+    g = x.to(T)
+    op.mfmg_qk_rope_bwd(plan, g, dx, dyd=g if dual else None, dxd=dxd)
+    for t in (y, yd, dx, dxd):
+        if t is not None:
+            assert torch.equal(t == float("inf"), at) and torch.isfinite(t[~at]).all()
