@@ -37,9 +37,6 @@ __device__ __forceinline__ f32x4 load4(const bf16_t* p) {
   return f32x4{__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u),
                __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u)};
 }
-__device__ __forceinline__ float load1(const float* p) { return *p; }
-__device__ __forceinline__ float load1(const bf16_t* p) { return bf2f(*p); }
-
 // Sum over the LPH lanes of a head, in all of them: quads, halves and rows of 16 lanes by
 // DPP (each step adds what the mirrored lane holds of the other half), row pairs by
 // exchanging rows.
@@ -68,31 +65,30 @@ __device__ __forceinline__ void put4(float* p, const f32x4& v) { store4(p, v[0],
 __device__ __forceinline__ void put4(bf16_t* p, const f32x4& v) { store4(p, v[0], v[1], v[2], v[3]); }
 
 // Rotation of a lane's dims d .. d + 3 of a head: z_k = y_k c_k + y'_k s_k with y' the
-// pairs' other members (back: the transpose has -s).
+// pairs' other members (back: the transpose has -s), which the lane or another of the
+// head's holds.
 template <int LPH>
 struct Rot {
   f32x4 c, s;
   double f4[4];   // quarter turns per position (0 past the rotated dims)
-  int other[4];   // dims of y'
-  int how;        // where y' is: 0 the lane's own (interleaved), 1 the lane LPH / 2 away
-                  // (the whole head, LPH lanes), 2 four dims in memory, 3 any dims
+  int how;        // where y' is: 0 in the lane (interleaved), 1 in the lane LPH / 2 away
+                  // (the whole head, LPH lanes), 2 in one other lane, 3 in any
   int rotated;    // dims of the lane's (first ones) that rotate: < 1 none, > 3 all; the others'
                   // y' is 0, so that an infinity passes as one
+  int half;
   unsigned first; // bit k: dim k is its pair's first member
 
   __device__ __forceinline__ void init(const RopeFreqs& f, int d) {
-    const int half = f.dims >> 1;
+    half = f.dims >> 1;
     how = f.interleaved ? 0 : LPH >= 16 && f.dims == 4 * LPH ? 1 : (f.dims & 7) == 0 ? 2 : 3;
-    first = 0;
     rotated = f.dims - d;
+    first = 0;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const int j = d + k;
-      other[k] = j;
       f4[k] = 0.0;
       if (j < f.dims) {
         const bool one = f.interleaved ? !(j & 1) : j < half;
-        other[k] = f.interleaved ? j ^ 1 : one ? j + half : j - half;
         f4[k] = f.f4[f.interleaved ? j >> 1 : one ? j : j - half];
         first |= (unsigned)one << k;
       }
@@ -115,31 +111,36 @@ struct Rot {
       s[k] = first >> k & 1 ? -(ss * m) : ss * m;
     }
   }
-  // y' of a head in memory, where the lanes do not hold it
-  template <typename T>
-  __device__ __forceinline__ f32x4 fetch(const T* head) const {
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    if (how == 2 && rotated > 0) v = load4(head + other[0]);
-    if (how == 3) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (k < rotated) v[k] = load1(head + other[k]);
-    }
-    return v;
-  }
-  // y' from the lanes' own values, or as fetched
-  __device__ __forceinline__ f32x4 pairs(const f32x4& own, const f32x4& fetched) const {
+  __device__ __forceinline__ f32x4 pairs(const f32x4& own) const {
+    const auto keep = [](float v, int m) { return __builtin_bit_cast(float, __builtin_bit_cast(int, v) & m); };
     if (how == 0) {
-      const bool a = rotated > 0, b = rotated > 2;
-      return f32x4{a ? own[1] : 0.f, a ? own[0] : 0.f, b ? own[3] : 0.f, b ? own[2] : 0.f};
+      const int a = rotated > 0 ? -1 : 0, b = rotated > 2 ? -1 : 0;
+      return f32x4{keep(own[1], a), keep(own[0], a), keep(own[3], b), keep(own[2], b)};
     }
+    f32x4 v;
     if (how == 1) {
-      f32x4 v;
 #pragma unroll
       for (int k = 0; k < 4; ++k) v[k] = LPH == 32 ? swap16(own[k]) : dpp<0x128>(own[k]);   // row_ror 8
       return v;
     }
-    return fetched;
+    const auto of = [](int lane, float x) {
+      return __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(4 * lane, __builtin_bit_cast(int, x)));
+    };
+    const int lane = threadIdx.x & 63;
+    if (how == 2) {   // (half is a multiple of 4, and the lane's dims rotate all or none)
+      const int m = rotated > 0 ? -1 : 0, l = lane + ((first ? half >> 2 : -(half >> 2)) & m);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = keep(of(l, own[k]), m);
+      return v;
+    }
+    const auto at = [&](int e) { e &= 3; return e == 0 ? own[0] : e == 1 ? own[1] : e == 2 ? own[2] : own[3]; };
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {   // element k + half of a later lane, or k - half of an earlier one
+      const float x = of(k < rotated ? lane + ((k + half) >> 2) : lane, at(k + half));
+      const float y = of(k < rotated ? lane + ((k - half) >> 2) : lane, at(k - half));
+      v[k] = k >= rotated ? 0.f : first >> k & 1 ? x : y;
+    }
+    return v;
   }
 };
 
@@ -160,35 +161,25 @@ __global__ void __launch_bounds__(64 * WAVES) qk_rope_fwd_kernel(QkRopeArgs<T> a
   Rot<LPH> rot;
   rot.init(a.f, d);
   struct Row {
-    f32x4 v, p, vd, pd;
+    f32x4 v, vd;
   };
   auto load = [&](int h) {
-    Row r = {none, none, none, none};
+    Row r = {none, none};
     if (live && h < nh) {
-      const float* x = a.x + tok * a.ldx + (long)h * dh;
-      r.v = load4(x + d);
-      if (rot.how > 1) r.p = rot.fetch(x);
-      if constexpr (DUAL) {
-        const float* xd = a.xd + tok * a.ldxd + (long)h * dh;
-        r.vd = load4(xd + d);
-        if (rot.how > 1) r.pd = rot.fetch(xd);
-      }
+      r.v = load4(a.x + tok * a.ldx + (long)h * dh + d);
+      if constexpr (DUAL) r.vd = load4(a.xd + tok * a.ldxd + (long)h * dh + d);
     }
     return r;
   };
   int h = (int)(item % splits) * HP + sub;
   Row cur = load(h);
   rot.at(a.f, d, a.p.pos[tok]);
-  f32x4 g[2], gp[2], gd[2], gdp[2];   // q, k gains and those of the pairs' other members
+  f32x4 g[2], gd[2];   // q, k gains
   if constexpr (NORM) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       g[k] = live ? load4(a.gain + k * dh + d) : none;
-      gp[k] = rot.pairs(g[k], live ? rot.fetch(a.gain + k * dh) : none);
-      if constexpr (DUAL) {
-        gd[k] = live ? load4(a.gaind + k * dh + d) : none;
-        gdp[k] = rot.pairs(gd[k], live ? rot.fetch(a.gaind + k * dh) : none);
-      }
+      if constexpr (DUAL) gd[k] = live ? load4(a.gaind + k * dh + d) : none;
     }
   }
   const float inv = 1.0f / dh;
@@ -196,23 +187,18 @@ __global__ void __launch_bounds__(64 * WAVES) qk_rope_fwd_kernel(QkRopeArgs<T> a
     const Row next = load(h + step);
     f32x4 v = cur.v, vd = cur.vd;
     if (h < nrot) {
-      f32x4 p = rot.pairs(v, cur.p), pd = none;
-      if constexpr (DUAL) pd = rot.pairs(vd, cur.pd);
       if constexpr (NORM) {
         const bool k = h >= a.H;
-        const f32x4 w = k ? g[1] : g[0], wp = k ? gp[1] : gp[0];
+        const f32x4 w = k ? g[1] : g[0];
         const float r = rsqrtf(head_sum<LPH>(sum4(v * v)) * inv + a.eps);
         if constexpr (DUAL) {
-          const f32x4 wd = k ? gd[1] : gd[0], wdp = k ? gdp[1] : gdp[0];
           const float c = r * head_sum<LPH>(sum4(v * vd)) * inv;
-          vd = wd * (r * v) + w * (r * (vd - c * (r * v)));
-          pd = wdp * (r * p) + wp * (r * (pd - c * (r * p)));
+          vd = (k ? gd[1] : gd[0]) * (r * v) + w * (r * (vd - c * (r * v)));
         }
         v = w * (r * v);
-        p = wp * (r * p);
       }
-      v = v * rot.c + p * rot.s;
-      if constexpr (DUAL) vd = vd * rot.c + pd * rot.s;
+      v = v * rot.c + rot.pairs(v) * rot.s;
+      if constexpr (DUAL) vd = vd * rot.c + rot.pairs(vd) * rot.s;
     }
     if (live) {
       put4(a.y + tok * a.ldy + (long)h * dh + d, v);
@@ -251,23 +237,17 @@ __global__ void __launch_bounds__(64 * WAVES) qk_rope_bwd_kernel(QkRopeArgs<T> a
   Rot<LPH> rot;
   rot.init(a.f, d);
   struct Row {
-    f32x4 v, p, vd, pd, x, xd;
+    f32x4 v, vd, x, xd;
   };
   for (long item = (long)blockIdx.x * WAVES + w; item < a.p.n * splits;
        item += (long)gridDim.x * WAVES) {
     const long tok = item / splits;
     if (tok < first || tok >= last) continue;
     auto load = [&](int h) {
-      Row r = {none, none, none, none, none, none};
+      Row r = {none, none, none, none};
       if (live && h < nh) {
-        const T* y = a.y + tok * a.ldy + (long)h * dh;
-        r.v = load4(y + d);
-        if (rot.how > 1) r.p = rot.fetch(y);
-        if constexpr (DUAL) {
-          const T* yd = a.yd + tok * a.ldyd + (long)h * dh;
-          r.vd = load4(yd + d);
-          if (rot.how > 1) r.pd = rot.fetch(yd);
-        }
+        r.v = load4(a.y + tok * a.ldy + (long)h * dh + d);
+        if constexpr (DUAL) r.vd = load4(a.yd + tok * a.ldyd + (long)h * dh + d);
         if constexpr (NORM) {
           if (h < nrot) {
             r.x = load4(a.x + tok * a.ldx + (long)h * dh + d);
@@ -284,8 +264,8 @@ __global__ void __launch_bounds__(64 * WAVES) qk_rope_bwd_kernel(QkRopeArgs<T> a
       const Row next = load(h + step);
       f32x4 v = cur.v, vd = cur.vd;
       if (h < nrot) {
-        v = v * rot.c - rot.pairs(v, cur.p) * rot.s;
-        if constexpr (DUAL) vd = vd * rot.c - rot.pairs(vd, cur.pd) * rot.s;
+        v = v * rot.c - rot.pairs(v) * rot.s;
+        if constexpr (DUAL) vd = vd * rot.c - rot.pairs(vd) * rot.s;
         if constexpr (NORM) {
           const bool k = h >= a.H;
           const f32x4 e = (k ? g[1] : g[0]) * v;
