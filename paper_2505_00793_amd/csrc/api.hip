@@ -1478,7 +1478,7 @@ mfmg_status run_rope_bwd(QkRopeArgs<T> r, const void* dy, const void* dyd, int64
     P.grad_out = dgain;
     P.hvp_out = dgaind;
     int sums = 0;
-    const float* p = qk_rope_sums(r.partial, r.p.n, r.H, r.K, r.dh, &sums);
+    const float* p = qk_rope_sums(r.partial, r.p.n, r.H, r.K, r.dh, r.dual, &sums);
     HIPCHK(gain_param<T>(p, sums, r.dh, 0, r.dh, P, nullptr, nullptr, s));
   } else if (r.gain) {
     HIPCHK(fill(dgain, 2 * r.dh, 0.f, s));

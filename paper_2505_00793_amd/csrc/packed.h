@@ -115,10 +115,10 @@ struct QkRopeArgs {
 template <typename T>
 hipError_t qk_rope_fwd(const QkRopeArgs<T>& a, hipStream_t s);
 // Writes dx (dxd) and, with norms, partial sums of the gains' gradients (q, k, and their
-// tangents): qk_rope_partials rows of [4][dh], of which qk_rope_sums says which `count`
+// tangents): qk_rope_partials rows of [4][dh] (dual: no more), of which qk_rope_sums says which `count`
 // gain_param finishes.
 int qk_rope_partials(long n, int H, int K, int dh);
-const float* qk_rope_sums(const float* partial, long n, int H, int K, int dh, int* count);
+const float* qk_rope_sums(const float* partial, long n, int H, int K, int dh, bool dual, int* count);
 template <typename T>
 hipError_t qk_rope_bwd(const QkRopeArgs<T>& a, hipStream_t s);
 // The parameter epilogue on column sums of partial [parts][4][d] (transformer.hip).

@@ -28,8 +28,13 @@ namespace mfmg {
 
 namespace {
 
-constexpr int WAVES = 4;          // of a workgroup
-constexpr int MAX_PARTS = 1024;   // workgroups of a backward that sums gains
+constexpr int WAVES = 4;   // of a workgroup
+// Workgroups of a backward that sums gains: what its registers let the 256 CUs hold at once
+// (5 and 3 waves a SIMD), so that all go through the rows together.  Dual, 8191 tokens of
+// 16 + 2 heads of 128: 512 132, 768 117, 1024 128 us with the forward; primal, 65536
+// tokens of 32 + 8: 768 1106, 1024 1054, 1280 1050.  (Fewer workgroups of 12 and 10 waves
+// leave fewer partial sums, but wait for each other: 119 and 1200.)
+constexpr int max_parts(bool dual) { return dual ? 768 : 1280; }
 
 __device__ __forceinline__ f32x4 load4(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
 __device__ __forceinline__ f32x4 load4(const bf16_t* p) {
@@ -329,17 +334,19 @@ __global__ void __launch_bounds__(256) gain_group_kernel(const float* __restrict
 
 int lanes_per_head(int dh) { return dh <= 32 ? 8 : dh <= 64 ? 16 : 32; }
 
-// Waves of one token: its groups of heads are dealt to more waves while there are too
-// few tokens to fill the chip.
+// Waves of one token: its groups of heads are dealt evenly to more waves while there are too
+// few tokens to fill the chip (999 tokens of 10 + 5 heads of 80, dual: up to 8192 waves 31 us,
+// 4096 27.5, 2048 27.1, where each forms the angles anew; 256 tokens the same either way).
 int splits_of(long n, int H, int K, int dh) {
   const int hp = 64 / lanes_per_head(dh), groups = (H + 2 * K + hp - 1) / hp;
   int s = 1;
-  while (s < groups && n * s < 8192) s *= 2;
-  return std::min(s, groups);
+  while (s < groups && n * s < 2048) s *= 2;
+  const int per = (groups + s - 1) / s;
+  return (groups + per - 1) / per;
 }
-int bwd_blocks(long n, int H, int K, int dh) {   // (with norms)
+int bwd_blocks(long n, int H, int K, int dh, bool dual) {   // (with norms)
   const long items = n * splits_of(n, H, K, dh);
-  return (int)std::min((long)MAX_PARTS, std::max(1L, (items + WAVES - 1) / WAVES));
+  return (int)std::min((long)max_parts(dual), std::max(1L, (items + WAVES - 1) / WAVES));
 }
 
 // Few partials are left as they are.
@@ -349,7 +356,7 @@ template <typename T, int LPH, bool NORM, bool DUAL>
 hipError_t launch(const QkRopeArgs<T>& a, bool bwd, hipStream_t s) {
   const int splits = splits_of(a.p.n, a.H, a.K, a.dh);
   if (bwd) {
-    const int blocks = NORM ? bwd_blocks(a.p.n, a.H, a.K, a.dh)
+    const int blocks = NORM ? bwd_blocks(a.p.n, a.H, a.K, a.dh, DUAL)
                             : (int)((a.p.n * splits + WAVES - 1) / WAVES);
     hipLaunchKernelGGL((qk_rope_bwd_kernel<T, LPH, NORM, DUAL>), dim3(blocks), dim3(64 * WAVES), 0,
                        s, a, splits);
@@ -440,11 +447,11 @@ RopeFreqs rope_freqs(const mfmg_attn_desc& d) {
 }
 
 int qk_rope_partials(long n, int H, int K, int dh) {
-  const int parts = bwd_blocks(n, H, K, dh);
+  const int parts = bwd_blocks(n, H, K, dh, false);
   return parts + gain_groups(parts);
 }
-const float* qk_rope_sums(const float* partial, long n, int H, int K, int dh, int* count) {
-  const int parts = bwd_blocks(n, H, K, dh);
+const float* qk_rope_sums(const float* partial, long n, int H, int K, int dh, bool dual, int* count) {
+  const int parts = bwd_blocks(n, H, K, dh, dual);
   *count = gain_groups(parts);
   return *count < parts ? partial + (long)parts * 4 * dh : partial;
 }

@@ -1020,7 +1020,7 @@ struct TfEng {
         HC(qk_rope_bwd(r, s));
         if (y.norm) {
           int sums = 0;
-          const float* p = qk_rope_sums(a.qkpart, N, H, y.K, dh, &sums);
+          const float* p = qk_rope_sums(a.qkpart, N, H, y.K, dh, dual, &sums);
           HC(gain_param<T>(p, sums, dh, y.qkg[b], y.qkg[b] + dh, P, out ? out->qk[b] : nullptr,
                            out ? out->qk[b] + dh : nullptr, s));
         }
