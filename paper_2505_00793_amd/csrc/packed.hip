@@ -80,56 +80,57 @@ template <typename T, int DH>
 struct Tile {
   static constexpr int P = DH <= 64 ? 64 : 128;          // row pitch
   static constexpr int VE = Elem<T>::VE, NC = P / VE;    // chunks of a row
-  __device__ static __forceinline__ int at(int row, int chunk) {
+  __device__ static __forceinline__ int chunk(int row, int place) {   // and the place of a chunk
     const int x = (row >> 2) & 3, h = ((x ^ (x >> 1)) & 1) << 1 | x >> 1;   // 0, 2, 3, 1
     const int f = sizeof(T) == 4 ? row & 15 : NC >= 16 ? (row & 3) << 2 | h : ((row >> 1) & 1) << 2 | h;
-    return row * P + ((chunk ^ f) * VE);
+    return place ^ f;
   }
+  __device__ static __forceinline__ int at(int row, int c) { return row * P + chunk(row, c) * VE; }
 };
 
-// A block of KB rows (of the NT threads' workgroup) on its way through registers: the next
-// block is requested before the current one's products and stored to the other LDS
-// buffer after them.  A thread's chunks are NT / (chunks of a row) rows apart, so one
-// 32-bit offset serves them all (leading dimensions are below 2^22).  Columns past dh
-// repeat the row's last chunk: the other operand holds zeros there, or the results of
-// those columns are not stored.
-typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+// A block of KB rows on its way to an LDS tile: the NT threads of a workgroup load 16 bytes
+// each, straight to LDS, where a wave's 64 chunks land behind one another: a thread's chunk
+// is the one that the swizzle puts at its place.  No registers hold the data, and the next
+// block travels during the current one's products.  The compiler lets LDS reads pass such
+// loads only where it knows them to be of different variables, so a tile's two buffers
+// are two variables.  A thread's chunks are STEP rows apart (leading dimensions are below
+// 2^22: 32-bit offsets in a block).  Columns past dh repeat the row's last chunk: the other
+// operand holds zeros there, or the results of those columns are not stored.  Rows past
+// `last` are out of the descriptor's range and land as zeros.
+typedef __attribute__((address_space(3))) void lds_void;
+__device__ __forceinline__ void load_lds16(__amdgpu_buffer_rsrc_t rsrc, void* lds, unsigned off) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)lds, 16, off, 0, 0, 0);
+}
 template <typename T, int DH, int KB, int NT>
 struct Block {
   typedef Tile<T, DH> L;
-  static constexpr int N = KB * L::NC / NT, STEP = NT / L::NC;
-  static_assert(KB * L::NC % NT == 0 && NT % L::NC == 0, "chunks of a thread");
-  u32x4 v[N];
-  unsigned off;   // byte offset of the thread's chunk in the block's first STEP rows
+  static constexpr int N = KB * L::NC / NT, STEP = NT / L::NC, NO = STEP % 16 ? 2 : 1;
+  static_assert(KB * L::NC % NT == 0 && NT % L::NC == 0 && STEP % 8 == 0, "chunks of a thread");
+  unsigned off[NO];   // byte offset of the thread's chunk in the block's first (NO) STEP rows
   unsigned ldb;
   __device__ __forceinline__ void init(long ld, int dh, int tid) {
     ldb = (unsigned)ld * sizeof(T);
-    off = (tid / L::NC) * ldb + min(tid % L::NC, dh / L::VE - 1) * 16;
-  }
-  // rows row0 .. of g; rows past `last` read as row `last`
-  __device__ __forceinline__ void load(const T* __restrict__ g, int row0, int last, int tid) {
-    const char* p = reinterpret_cast<const char*>(g) + (long)row0 * ldb;
-    if (row0 + KB - 1 <= last) {
 #pragma unroll
-      for (int k = 0; k < N; ++k)
-        v[k] = *reinterpret_cast<const u32x4*>(p + (long)k * STEP * ldb + off);
-    } else {
-      const unsigned r = tid / L::NC, c = off - r * ldb;
-#pragma unroll
-      for (int k = 0; k < N; ++k)
-        v[k] = *reinterpret_cast<const u32x4*>(p + min(r + k * STEP, (unsigned)(last - row0)) * ldb + c);
+    for (int k = 0; k < NO; ++k) {   // (the swizzle repeats every 16 rows)
+      const int r = tid / L::NC + k * STEP;
+      off[k] = r * ldb + min(L::chunk(r, tid % L::NC), dh / L::VE - 1) * 16;
     }
   }
-  __device__ __forceinline__ void store(T* lds, int tid) const {
+  // rows row0 .. of g to the tile at lds, by wave w
+  __device__ __forceinline__ void load(const T* __restrict__ g, int row0, int last, T* lds, int w) const {
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<char*>(reinterpret_cast<const char*>(g) + (long)row0 * ldb), 0,
+        (int)(min(last - row0 + 1, KB) * ldb), 0x00020000);
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-      // (the swizzle repeats every 16 rows)
-      const int a = STEP % 16 ? L::at(tid / L::NC + k * STEP, tid % L::NC)
-                              : L::at(tid / L::NC, tid % L::NC) + k * STEP * L::P;
-      *reinterpret_cast<u32x4*>(lds + a) = v[k];
-    }
+    for (int k = 0; k < N; ++k)
+      load_lds16(rsrc, lds + (k * NT + w * 64) * L::VE, off[k % NO] + k / NO * NO * STEP * ldb);
   }
 };
+// Every wave's loads have landed, and nobody reads the other buffers any more.
+__device__ __forceinline__ void landed() {
+  __builtin_amdgcn_s_waitcnt(7 << 4);   // vmcnt(0) lgkmcnt(0)
+  __syncthreads();
+}
 
 // Fragment c of a row in global memory: elements FE (NG c + g) .. + FE - 1, zero past dh.
 template <int NG>
@@ -263,12 +264,12 @@ __device__ __forceinline__ void store_row(T* row, const V (&acc)[NE], float f, i
 // together; `lds` is free for it.
 template <int R, int NE, int KS>
 struct Merge {
-  static constexpr int AV = R * R / 64, LANE = NE * AV + 3;   // floats of a lane: an array, 3 scalars
+  static constexpr int AV = R * R / 64, LANE = NE * AV;   // floats of a lane
   float* p;
   int rank;   // 0 .. KS - 1
   __device__ __forceinline__ Merge(float* lds, int w, int lane)
       : p(lds + w / KS * LANE * 64 + lane), rank(w % KS) {}
-  __device__ __forceinline__ float& scalar(int i) { return p[(NE * AV + i) * 64]; }
+  __device__ __forceinline__ float& scalar(int i) { return p[i * 64]; }
   // from wave j: v of the first wave becomes v f0 + v_j f1
   template <typename V>
   __device__ __forceinline__ void add(int j, V (&v)[NE], float f0, float f1) {
@@ -314,8 +315,8 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<
   typedef typename AccT<R>::V V;
   typedef typename FragT<T>::V F;
   typedef Tile<T, DH> L;
-  __shared__ __attribute__((aligned(16))) T sK[2][KB * L::P], sV[2][KB * L::P],
-      sKd[DUAL ? 2 : 1][DUAL ? KB * L::P : 8], sVd[DUAL ? 2 : 1][DUAL ? KB * L::P : 8];
+  __shared__ __attribute__((aligned(16))) T sK0[KB * L::P], sK1[KB * L::P], sV0[KB * L::P], sV1[KB * L::P],
+      sKd0[DUAL ? KB * L::P : 8], sKd1[DUAL ? KB * L::P : 8], sVd0[DUAL ? KB * L::P : 8], sVd1[DUAL ? KB * L::P : 8];
   int rank, h;
   tile_of(a.H, rank, h);
   const TileList tl = a.p.list[tile_kind(ROWS)];
@@ -352,30 +353,23 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<
     rKd.init(a.ldkd, dh, tid);
     rVd.init(a.ldvd, dh, tid);
   }
-  auto load = [&](int k0) {
-    rK.load(K, k0, hi - 1, tid);
-    rV.load(Vp, k0, hi - 1, tid);
+  auto load = [&](int k0, auto buffer) {
+    constexpr bool b = decltype(buffer)::value;
+    rK.load(K, k0, hi - 1, b ? sK1 : sK0, w);
+    rV.load(Vp, k0, hi - 1, b ? sV1 : sV0, w);
     if constexpr (DUAL) {
-      rKd.load(Kd, k0, hi - 1, tid);
-      rVd.load(Vd, k0, hi - 1, tid);
-    }
-  };
-  auto store = [&](int b) {
-    rK.store(sK[b], tid);
-    rV.store(sV[b], tid);
-    if constexpr (DUAL) {
-      rKd.store(sKd[b], tid);
-      rVd.store(sVd[b], tid);
+      rKd.load(Kd, k0, hi - 1, b ? sKd1 : sKd0, w);
+      rVd.load(Vd, k0, hi - 1, b ? sVd1 : sVd0, w);
     }
   };
   const int nb = (min(tile.x + ROWS, hi) - 1 - lo) / KB + 1;
-  load(lo);
-  store(0);
+  load(lo, std::false_type());
   auto block = [&](int kb, auto buffer) {
-    constexpr int b = decltype(buffer)::value;
-    __syncthreads();   // block kb is in its buffer, and nobody reads the other one
+    constexpr bool b = decltype(buffer)::value;
+    const T *sK = b ? sK1 : sK0, *sV = b ? sV1 : sV0, *sKd = b ? sKd1 : sKd0, *sVd = b ? sVd1 : sVd0;
+    landed();   // block kb is in its buffer
     const int k0 = lo + kb * KB;
-    if (kb + 1 < nb) load(k0 + KB);
+    if (kb + 1 < nb) load(k0 + KB, std::bool_constant<!b>());
 #pragma unroll
     for (int sb = 0; sb < KB / SB; ++sb) {
       const int ks = k0 + sb * SB;
@@ -389,11 +383,11 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<
         if constexpr (DUAL) zero(sd[n]);
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-          const F kf = at.frag(sK[b], sb * SB + n * R, c);
+          const F kf = at.frag(sK, sb * SB + n * R, c);
           s[n] = mma(kf, qf[c], s[n]);
           if constexpr (DUAL) {
             sd[n] = mma(kf, qdf[c], sd[n]);
-            sd[n] = mma(at.frag(sKd[b], sb * SB + n * R, c), qf[c], sd[n]);
+            sd[n] = mma(at.frag(sKd, sb * SB + n * R, c), qf[c], sd[n]);
           }
         }
       }
@@ -438,25 +432,24 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<
         if constexpr (DUAL) pack(sd, c, pdf);
 #pragma unroll
         for (int e = 0; e < NE; ++e) {
-          const F vf = at.tfrag(sV[b], e, sb * NK + c);
+          const F vf = at.tfrag(sV, e, sb * NK + c);
           o[e] = mma(vf, pf, o[e]);
           if constexpr (DUAL) {
             od[e] = mma(vf, pdf, od[e]);
-            od[e] = mma(at.tfrag(sVd[b], e, sb * NK + c), pf, od[e]);
+            od[e] = mma(at.tfrag(sVd, e, sb * NK + c), pf, od[e]);
           }
         }
       }
     }
-    if (kb + 1 < nb) store(b ^ 1);
   };
   for (int kb = 0; kb < nb; kb += 2) {   // (buffers at constant addresses)
-    block(kb, std::integral_constant<int, 0>());
-    if (kb + 1 < nb) block(kb + 1, std::integral_constant<int, 1>());
+    block(kb, std::false_type());
+    if (kb + 1 < nb) block(kb + 1, std::true_type());
   }
   if constexpr (KS > 1) {
     // the other waves' keys join in, at the larger maximum
-    Merge<R, NE, KS> M(reinterpret_cast<float*>(&sK[0][0]), w, lane);
-    static_assert(NW / KS * M.LANE * 256 <= sizeof(sK), "merge buffer");
+    Merge<R, NE, KS> M(reinterpret_cast<float*>(sK0), w, lane);
+    static_assert(NW / KS * M.LANE * 256 <= sizeof(sK0), "merge buffer");
 #pragma unroll
     for (int j = 1; j < KS; ++j) {
       __syncthreads();
@@ -516,8 +509,8 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T
   typedef typename AccT<R>::V V;
   typedef typename FragT<T>::V F;
   typedef Tile<T, DH> L;
-  __shared__ __attribute__((aligned(16))) T sK[2][KB * L::P], sV[2][KB * L::P],
-      sKd[DUAL ? 2 : 1][DUAL ? KB * L::P : 8], sVd[DUAL ? 2 : 1][DUAL ? KB * L::P : 8];
+  __shared__ __attribute__((aligned(16))) T sK0[KB * L::P], sK1[KB * L::P], sV0[KB * L::P], sV1[KB * L::P],
+      sKd0[DUAL ? KB * L::P : 8], sKd1[DUAL ? KB * L::P : 8], sVd0[DUAL ? KB * L::P : 8], sVd1[DUAL ? KB * L::P : 8];
   int rank, h;
   tile_of(a.H, rank, h);
   const TileList tl = a.p.list[tile_kind(ROWS)];
@@ -570,30 +563,23 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T
     rKd.init(a.ldkd, dh, tid);
     rVd.init(a.ldvd, dh, tid);
   }
-  auto load = [&](int k0) {
-    rK.load(K, k0, hi - 1, tid);
-    rV.load(Vp, k0, hi - 1, tid);
+  auto load = [&](int k0, auto buffer) {
+    constexpr bool b = decltype(buffer)::value;
+    rK.load(K, k0, hi - 1, b ? sK1 : sK0, w);
+    rV.load(Vp, k0, hi - 1, b ? sV1 : sV0, w);
     if constexpr (DUAL) {
-      rKd.load(Kd, k0, hi - 1, tid);
-      rVd.load(Vd, k0, hi - 1, tid);
-    }
-  };
-  auto store = [&](int b) {
-    rK.store(sK[b], tid);
-    rV.store(sV[b], tid);
-    if constexpr (DUAL) {
-      rKd.store(sKd[b], tid);
-      rVd.store(sVd[b], tid);
+      rKd.load(Kd, k0, hi - 1, b ? sKd1 : sKd0, w);
+      rVd.load(Vd, k0, hi - 1, b ? sVd1 : sVd0, w);
     }
   };
   const int nb = (min(tile.x + ROWS, hi) - 1 - lo) / KB + 1;
-  load(lo);
-  store(0);
+  load(lo, std::false_type());
   auto block = [&](int kb, auto buffer) {
-    constexpr int b = decltype(buffer)::value;
-    __syncthreads();
+    constexpr bool b = decltype(buffer)::value;
+    const T *sK = b ? sK1 : sK0, *sV = b ? sV1 : sV0, *sKd = b ? sKd1 : sKd0, *sVd = b ? sVd1 : sVd0;
+    landed();
     const int k0 = lo + kb * KB;
-    if (kb + 1 < nb) load(k0 + KB);
+    if (kb + 1 < nb) load(k0 + KB, std::bool_constant<!b>());
 #pragma unroll
     for (int sb = 0; sb < KB / SB; ++sb) {
       const int ks = k0 + sb * SB;
@@ -609,14 +595,14 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
           const int kr = sb * SB + n * R;
-          const F kf = at.frag(sK[b], kr, c), vf = at.frag(sV[b], kr, c);
+          const F kf = at.frag(sK, kr, c), vf = at.frag(sV, kr, c);
           s = mma(kf, qf[c], s);
           dp = mma(vf, gf[c], dp);
           if constexpr (DUAL) {
             sd = mma(kf, qdf[c], sd);
-            sd = mma(at.frag(sKd[b], kr, c), qf[c], sd);
+            sd = mma(at.frag(sKd, kr, c), qf[c], sd);
             dpd = mma(vf, gdf[c], dpd);
-            dpd = mma(at.frag(sVd[b], kr, c), gf[c], dpd);
+            dpd = mma(at.frag(sVd, kr, c), gf[c], dpd);
           }
         }
         if (diag) {   // some key may follow some query: its weight is 2^-inf = 0
@@ -642,24 +628,23 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T
         if constexpr (DUAL) pack(dsd, c, ddf);
 #pragma unroll
         for (int e = 0; e < NE; ++e) {
-          const F kt = at.tfrag(sK[b], e, sb * NK + c);
+          const F kt = at.tfrag(sK, e, sb * NK + c);
           dq[e] = mma(kt, df, dq[e]);
           if constexpr (DUAL) {
             dqd[e] = mma(kt, ddf, dqd[e]);
-            dqd[e] = mma(at.tfrag(sKd[b], e, sb * NK + c), df, dqd[e]);
+            dqd[e] = mma(at.tfrag(sKd, e, sb * NK + c), df, dqd[e]);
           }
         }
       }
     }
-    if (kb + 1 < nb) store(b ^ 1);
   };
   for (int kb = 0; kb < nb; kb += 2) {   // (buffers at constant addresses)
-    block(kb, std::integral_constant<int, 0>());
-    if (kb + 1 < nb) block(kb + 1, std::integral_constant<int, 1>());
+    block(kb, std::false_type());
+    if (kb + 1 < nb) block(kb + 1, std::true_type());
   }
   if constexpr (KS > 1) {
-    Merge<R, NE, KS> M(reinterpret_cast<float*>(&sK[0][0]), w, lane);
-    static_assert(NW / KS * M.LANE * 256 <= sizeof(sK), "merge buffer");
+    Merge<R, NE, KS> M(reinterpret_cast<float*>(sK0), w, lane);
+    static_assert(NW / KS * M.LANE * 256 <= sizeof(sK0), "merge buffer");
 #pragma unroll
     for (int j = 1; j < KS; ++j) {
       M.add(j, dq, 1.f, 1.f);
@@ -684,8 +669,8 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dkv_kernel(PackedAttnArgs<
   typedef typename AccT<R>::V V;
   typedef typename FragT<T>::V F;
   typedef Tile<T, DH> L;
-  __shared__ __attribute__((aligned(16))) T sQ[2][KB * L::P], sG[2][KB * L::P],
-      sQd[DUAL ? 2 : 1][DUAL ? KB * L::P : 8], sGd[DUAL ? 2 : 1][DUAL ? KB * L::P : 8];
+  __shared__ __attribute__((aligned(16))) T sQ0[KB * L::P], sQ1[KB * L::P], sG0[KB * L::P], sG1[KB * L::P],
+      sQd0[DUAL ? KB * L::P : 8], sQd1[DUAL ? KB * L::P : 8], sGd0[DUAL ? KB * L::P : 8], sGd1[DUAL ? KB * L::P : 8];
   __shared__ __attribute__((aligned(16))) float sL[2][KB], sR[2][KB], sC[2][KB], sRd[2][KB];
   int rank, hp;
   tile_of(a.K * a.parts, rank, hp);
@@ -729,13 +714,14 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dkv_kernel(PackedAttnArgs<
   }
   float xL = 0.f, xR = 0.f, xC = 0.f, xRd = 0.f;   // a query's row values (threads 0 .. 63)
   const int nq = (hi - tile.x + KB - 1) / KB, nb = nq * GP;
-  auto load = [&](int i) {   // block i: query head i / nq, its block i % nq
+  auto load = [&](int i, auto buffer) {   // block i: query head i / nq, its block i % nq
+    constexpr bool b = decltype(buffer)::value;
     const int hq = i / nq, h = h0 + hq, r0 = tile.x + (i - hq * nq) * KB;
-    rQ.load(a.q + (long)h * dh, r0, hi - 1, tid);
-    rG.load(a.g + (long)h * dh, r0, hi - 1, tid);
+    rQ.load(a.q + (long)h * dh, r0, hi - 1, b ? sQ1 : sQ0, w);
+    rG.load(a.g + (long)h * dh, r0, hi - 1, b ? sG1 : sG0, w);
     if constexpr (DUAL) {
-      rQd.load(a.qd + (long)h * dh, r0, hi - 1, tid);
-      rGd.load(a.gd + (long)h * dh, r0, hi - 1, tid);
+      rQd.load(a.qd + (long)h * dh, r0, hi - 1, b ? sQd1 : sQd0, w);
+      rGd.load(a.gd + (long)h * dh, r0, hi - 1, b ? sGd1 : sGd0, w);
     }
     const long x = (long)h * a.p.n + min(r0 + (tid & (KB - 1)), hi - 1);
     xL = a.lse[x];
@@ -746,12 +732,6 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dkv_kernel(PackedAttnArgs<
     }
   };
   auto store = [&](int b) {
-    rQ.store(sQ[b], tid);
-    rG.store(sG[b], tid);
-    if constexpr (DUAL) {
-      rQd.store(sQd[b], tid);
-      rGd.store(sGd[b], tid);
-    }
     if (tid < KB) {
       sL[b][tid] = xL;
       sR[b][tid] = xR;
@@ -761,13 +741,14 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dkv_kernel(PackedAttnArgs<
       }
     }
   };
-  load(0);
+  load(0, std::false_type());
   store(0);
   int r0 = tile.x;   // first query of the block
   auto block = [&](int i, auto buffer) {
-    constexpr int b = decltype(buffer)::value;
-    __syncthreads();
-    if (i + 1 < nb) load(i + 1);
+    constexpr bool b = decltype(buffer)::value;
+    const T *sQ = b ? sQ1 : sQ0, *sG = b ? sG1 : sG0, *sQd = b ? sQd1 : sQd0, *sGd = b ? sGd1 : sGd0;
+    landed();
+    if (i + 1 < nb) load(i + 1, std::bool_constant<!b>());
 #pragma unroll
     for (int sb = 0; sb < KB / SB; ++sb) {
       const int qs = r0 + sb * SB;
@@ -783,14 +764,14 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dkv_kernel(PackedAttnArgs<
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
           const int qr = sb * SB + n * R;
-          const F qq = at.frag(sQ[b], qr, c), gg = at.frag(sG[b], qr, c);
+          const F qq = at.frag(sQ, qr, c), gg = at.frag(sG, qr, c);
           s = mma(qq, kf[c], s);
           dp = mma(gg, vf[c], dp);
           if constexpr (DUAL) {
             sd = mma(qq, kdf[c], sd);
-            sd = mma(at.frag(sQd[b], qr, c), kf[c], sd);
+            sd = mma(at.frag(sQd, qr, c), kf[c], sd);
             dpd = mma(gg, vdf[c], dpd);
-            dpd = mma(at.frag(sGd[b], qr, c), vf[c], dpd);
+            dpd = mma(at.frag(sGd, qr, c), vf[c], dpd);
           }
         }
         if (mask) {   // (weight 0, as above)
@@ -835,30 +816,30 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dkv_kernel(PackedAttnArgs<
         }
 #pragma unroll
         for (int e = 0; e < NE; ++e) {
-          const F gt = at.tfrag(sG[b], e, sb * NK + c);
-          const F qt = at.tfrag(sQ[b], e, sb * NK + c);
+          const F gt = at.tfrag(sG, e, sb * NK + c);
+          const F qt = at.tfrag(sQ, e, sb * NK + c);
           dv[e] = mma(gt, pf, dv[e]);
           dk[e] = mma(qt, df, dk[e]);
           if constexpr (DUAL) {
             dvd[e] = mma(gt, pdf, dvd[e]);
-            dvd[e] = mma(at.tfrag(sGd[b], e, sb * NK + c), pf, dvd[e]);
+            dvd[e] = mma(at.tfrag(sGd, e, sb * NK + c), pf, dvd[e]);
             dkd[e] = mma(qt, ddf, dkd[e]);
-            dkd[e] = mma(at.tfrag(sQd[b], e, sb * NK + c), df, dkd[e]);
+            dkd[e] = mma(at.tfrag(sQd, e, sb * NK + c), df, dkd[e]);
           }
         }
       }
     }
     r0 += KB;
     if (r0 >= hi) r0 = tile.x;
-    if (i + 1 < nb) store(b ^ 1);
+    if (i + 1 < nb) store(!b);
   };
   for (int i = 0; i < nb; i += 2) {
-    block(i, std::integral_constant<int, 0>());
-    if (i + 1 < nb) block(i + 1, std::integral_constant<int, 1>());
+    block(i, std::false_type());
+    if (i + 1 < nb) block(i + 1, std::true_type());
   }
   if constexpr (KS > 1) {
-    Merge<R, NE, KS> M(reinterpret_cast<float*>(&sQ[0][0]), w, lane);
-    static_assert(NW / KS * M.LANE * 256 <= sizeof(sQ), "merge buffer");
+    Merge<R, NE, KS> M(reinterpret_cast<float*>(sQ0), w, lane);
+    static_assert(NW / KS * M.LANE * 256 <= sizeof(sQ0), "merge buffer");
 #pragma unroll
     for (int j = 1; j < KS; ++j) {
       M.add(j, dk, 1.f, 1.f);
