@@ -299,8 +299,8 @@ __device__ __forceinline__ void tile_of(int heads, int& rank, int& head) {
 }
 
 // ---------------------------------------------------------------- forward
-// 16384 tokens of 16 heads of 128 over 2 key heads, bf16: 1.11 ms, 0.99 PFLOP/s (a bf16
-// product of 8192^3 reaches 1.21); dual, 2 x 4096 tokens of 8 heads of 64: 122 us, 0.84.
+// 16384 tokens of 16 heads of 128 over 2 key heads, bf16: 1.00 ms, 1.10 PFLOP/s (a bf16
+// product of 8192^3 reaches 1.21); dual, 2 x 4096 tokens of 8 heads of 64: 112 us, 0.92.
 // A workgroup owns NW R / KS queries of one head.  Scores are formed for SB keys at a time
 // and consumed before the next SB, which bounds the registers they need.  The running
 // maximum is only raised, and the accumulators rescaled, when a score exceeds it by
@@ -1020,17 +1020,24 @@ int dkv_parts(long n, int H, int K) {
 
 // Rows a wave owns, waves of a workgroup, waves that share rows, rows of a staged block, rows
 // of it that a wave forms and consumes scores of at a time, waves a SIMD holds, addresses
-// pinned (Lane).  What they were chosen by, in us:
-//  forward and dQ, 128 dims, bf16 (16001 tokens in 40 sequences of 16 heads | 16384 in one): 32 rows a
-//   wave, 4 waves, 104 | 1160 and 170; 16 rows, 4 waves 115 | 1380 and 178 (twice the LDS
-//   reads a product); 16 rows, 8 waves 110 | 1200 and 200;
-//  dK/dV, 128 dims: 16 rows, 4 waves 209; 16 rows, 8 waves 246; 32 rows need more
-//   registers than two waves a SIMD have (593 with spills, 246 with V in LDS);
-//  dual, 64 dims (2 x 4096 tokens of 8 heads): 16 rows, 8 waves 131, 167, 226 for the three
-//   passes; 4 waves 135, 193, 257; 32 rows 145, 232, 277;
-//  dual, 128 dims (8191 tokens of 12 heads): 16 rows, 4 waves, blocks of 32 and one wave a
-//   SIMD for dK/dV 165, 225, 379; 8 waves 165, 238, 1340 (spills); unpinned 165, 250, 410;
-//  float32: 16 rows, one wave a SIMD (dual 64 dims: 32 rows take twice the time);
+// pinned (Lane).  What they were chosen by, in us (the longer differences were measured
+// with blocks staged through registers, which cost all of them a tenth more):
+//  forward and dQ, 128 dims, bf16 (16001 tokens in 40 sequences of 16 heads | 16384 in one):
+//   32 rows a wave, 4 waves, 104 | 1160 and 170; 16 rows, 4 waves 115 | 1380 and 178 (twice
+//   the LDS reads a product); 16 rows, 8 waves 110 | 1200 and 200; blocks of 32 rows in the
+//   forward 1003, of 64 1048;
+//  dK/dV, 128 dims: 16 rows, 4 waves 209; 16 rows, 8 waves 246; 32 rows need more registers
+//   than two waves a SIMD have: with the V fragments in LDS 4 x 4096 tokens take 950 us for
+//   the whole backward, 1000 with 16 rows, but the 40 short sequences 368 and 340, whose
+//   tiles they fill less;
+//  dual, 64 dims (2 x 4096 tokens of 8 heads): 16 rows, 8 waves 112 and 344 (both backward
+//   passes); 4 waves, blocks of 32 109 and 359; 32 rows 145 and 509;
+//  dual, 128 dims (8191 tokens of 12 heads): dK/dV 16 rows, 4 waves, blocks of 64 and one wave
+//   a SIMD, the backward 558; blocks of 32 and two waves a SIMD 640 (spills), with fragments
+//   of the own rows in LDS 575; unpinned 580;
+//  float32: 16 rows, one wave a SIMD (dual 64 dims: 32 rows take twice the time), but dual
+//   up to 64 dims two waves and blocks of 32 (2 x 2048 tokens of 16 heads of 64: forward
+//   456 -> 430, backward 1537 -> 1495);
 //  few rows (bf16: 16 x 256 tokens of 8 heads, 64-row tiles 8.1, 9.6, 10.5, 128-row tiles 9.0,
 //   11.4, 15.4; float32: 1531 tokens of 6 heads, pairs of waves sharing 32 rows 62, 79, 105,
 //   64-row tiles 118, 166, 229).
@@ -1041,10 +1048,11 @@ struct Shape {
   static constexpr int R = !F32 && !DUAL && PASS != DKV && !SMALL ? 32 : 16;
   static constexpr int NW = !F32 && DUAL && !BIG && !SMALL ? 8 : 4;
   static constexpr int KS = F32 && SMALL ? 2 * SMALL : 1;
-  static constexpr int KB = BIG && (DUAL ? F32 || PASS != DKV : !F32 && PASS == FWD) ? 32 : 64;
+  static constexpr bool FEW = F32 && DUAL && !BIG && PASS != DKV && !SMALL;
+  static constexpr int KB = FEW || (BIG && (DUAL ? F32 || PASS != DKV : !F32 && PASS == FWD)) ? 32 : 64;
   static constexpr int SB = F32 && KB < 32 * KS ? 16 : 32;
-  static constexpr int MW = F32 || (DUAL && BIG && PASS == DKV) ? 1 : 2;
-  static constexpr bool PIN = F32 ? BIG && DUAL : BIG ? (DUAL ? PASS != FWD : PASS == FWD) : DUAL && SMALL;
+  static constexpr int MW = FEW ? 2 : F32 || (DUAL && BIG && PASS == DKV) ? 1 : 2;
+  static constexpr bool PIN = DUAL && BIG && (F32 || PASS != FWD);
   static constexpr int KIND = tile_kind(NW * R / KS);
 };
 
