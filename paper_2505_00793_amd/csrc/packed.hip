@@ -34,8 +34,8 @@
 // are formed again so that no sum needs atomics (a single pass would take 5 and 15 for
 // the backward, not 7 and 21).  They are fed from LDS, one fragment read a product and R
 // rows, by two or three waves a SIMD, whose exponentials run beside another's products.
-// Counters at 16384 tokens of 16 heads of 128: matrix units busy 48% of the cycles at the
-// 1.93 GHz the card then holds, vector units 49%, no bank conflicts.
+// Counters at 16384 tokens of 16 heads of 128: matrix units busy 64% of the cycles at the
+// 1.7 GHz the card then holds, vector units 50%, no bank conflicts.
 #include "packed.h"
 
 #include <algorithm>
@@ -499,8 +499,8 @@ __device__ __forceinline__ float dot(const f32x4& a, const f32x4& b) {
   return a[0] * b[0] + a[1] * b[1] + a[2] * b[2] + a[3] * b[3];
 }
 
-// 40 sequences of 16001 tokens in all, 16 heads of 128 over 2: 165 us, 0.56 PFLOP/s; dual, 2 x 4096
-// tokens of 8 heads of 64: 157 us, 0.98.  Score cotangents are formed without the scale s,
+// 40 sequences of 16001 tokens in all, 16 heads of 128 over 2: 152 us, 0.61 PFLOP/s; dual, 2 x 4096
+// tokens of 8 heads of 64: 142 us, 1.08.  Score cotangents are formed without the scale s,
 // which the sums take at the end.
 template <typename T, int DH, int R, int NW, int KS, int KB, int SB, int MW, bool PIN, bool DUAL>
 __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T> a) {
@@ -658,7 +658,7 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_dq_kernel(PackedAttnArgs<T
 }
 
 // ---------------------------------------------------------------- backward: dK, dV
-// The same calls: 209 us and 23 to add the parts, 0.54 PFLOP/s; dual 214 us, 0.96.
+// The same calls: 163 us and 23 to add the parts, 0.66 PFLOP/s; dual 194 us, 1.06.
 // A workgroup owns NW R / KS keys of one key head and goes through the queries of some of the
 // head's query heads (all, or one part of `parts`, whose float32 sums dkv_sum_kernel
 // adds in order).
