@@ -94,9 +94,8 @@ struct Tile {
 // block travels during the current one's products.  The compiler lets LDS reads pass such
 // loads only where it knows them to be of different variables, so a tile's two buffers
 // are two variables.  A thread's chunks are STEP rows apart (leading dimensions are below
-// 2^22: 32-bit offsets in a block).  Columns past dh repeat the row's last chunk: the other
-// operand holds zeros there, or the results of those columns are not stored.  Rows past
-// `last` are out of the descriptor's range and land as zeros.
+// 2^22: 32-bit offsets in a block, below 2^30).  Rows past `last` and columns past dh are out of
+// the descriptor's range and land as zeros.
 typedef __attribute__((address_space(3))) void lds_void;
 __device__ __forceinline__ void load_lds16(__amdgpu_buffer_rsrc_t rsrc, void* lds, unsigned off) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)lds, 16, off, 0, 0, 0);
@@ -112,8 +111,8 @@ struct Block {
     ldb = (unsigned)ld * sizeof(T);
 #pragma unroll
     for (int k = 0; k < NO; ++k) {   // (the swizzle repeats every 16 rows)
-      const int r = tid / L::NC + k * STEP;
-      off[k] = r * ldb + min(L::chunk(r, tid % L::NC), dh / L::VE - 1) * 16;
+      const int r = tid / L::NC + k * STEP, c = L::chunk(r, tid % L::NC);
+      off[k] = c < dh / L::VE ? r * ldb + c * 16 : 1u << 31;
     }
   }
   // rows row0 .. of g to the tile at lds, by wave w
@@ -1110,7 +1109,7 @@ hipError_t run(const PackedAttnArgs<T>& a, bool bwd, hipStream_t s) {
   return level ? run_at<T, DH, 1>(a, bwd, s) : run_at<T, DH, 0>(a, bwd, s);
 }
 // The products' head dimension: dh rounded up to one that is compiled (columns past dh are
-// zero in one operand, or not stored).
+// zero, and not stored).
 template <typename T>
 hipError_t run_dh(const PackedAttnArgs<T>& a, bool bwd, hipStream_t s) {
   if (a.dh <= 32) return run<T, 32>(a, bwd, s);

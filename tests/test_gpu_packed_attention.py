@@ -307,3 +307,52 @@ def test_few_long_float32_rows(dual, H, K, dh, lens):
     c = Call(0, H, K, dh, lens, dual, before=0, after=2).run()
     torch.cuda.synchronize()
     c.check()
+
+
+@pytest.mark.parametrize("prec", [0, 1], ids=["fp32", "bf16"])
+def test_widest_rows(prec):
+    """The largest leading dimension, 2^22: a block's rows span 2^30 bytes.  The same bits as from dense rows."""
+    print("\n[packed] rows 2^22 elements apart", flush=True)
+    M = _lib()
+    n, H, dh, ld = 131, 3, 128, 1 << 22
+    T = torch.bfloat16 if prec else torch.float32
+    op = M.Attention(M.make_attn_desc(heads=H, kv_heads=1, head_dim=dh, precision=prec))
+    plan = M.mfmg_seq_plan(torch.tensor([0, 70, 70, n], dtype=torch.int32, device="cuda"), n)
+    W, Q, gen = (H + 2) * dh, H * dh, torch.Generator(device="cuda").manual_seed(2)
+    wide = torch.empty(n, ld, device="cuda", dtype=T)
+    part = torch.randn(n, 2 * W + 2 * Q, device="cuda", generator=gen).to(T)
+    ws, out = op.workspace(n), []
+    for rows in (part.clone(), wide[:, :part.shape[1]].copy_(part)):
+        x, dx, o, g = rows.split((W, W, Q, Q), 1)
+        cut, stats = (Q, dh, dh), torch.empty(2, H, n, device="cuda")
+        op.mfmg_attn_fwd(plan, *x.split(cut, 1), o, stats)
+        op.mfmg_attn_bwd(plan, *x.split(cut, 1), o, stats, g, *dx.split(cut, 1), ws=ws)
+        torch.cuda.synchronize()
+        out.append(torch.cat((o, dx), 1))
+    assert torch.isfinite(out[0]).all() and torch.equal(*out)
+
+
+@pytest.mark.parametrize("prec", [0, 1], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("dh", [8, 72, 128])
+def test_a_key_at_minus_infinity_has_no_weight(prec, dh):
+    """Scores of -inf (keys 1, 5 and 40 hold -inf where every query holds 1) leave the other keys' result."""
+    print(f"\n[packed] keys at -inf, dh {dh}", flush=True)
+    M = _lib()
+    n, T = 70, torch.bfloat16 if prec else torch.float32
+    op = M.Attention(M.make_attn_desc(heads=1, kv_heads=1, head_dim=dh, precision=prec))
+    plan = M.mfmg_seq_plan(torch.tensor([0, n], dtype=torch.int32, device="cuda"), n)
+    gen = torch.Generator(device="cuda").manual_seed(dh)
+    q, k, v = (torch.randn(n, dh, device="cuda", generator=gen).to(T) for _ in range(3))
+    q[:, -1] = 1
+    k[[1, 5, 40], -1] = float("-inf")
+    o, stats = torch.empty(n, dh, device="cuda", dtype=T), torch.empty(2, 1, n, device="cuda")
+    op.mfmg_attn_fwd(plan, q, k, v, o, stats)
+    torch.cuda.synchronize()
+    s = (q.double() @ k.double().t()) * dh ** -0.5
+    p = torch.softmax(s.masked_fill(torch.ones_like(s).triu(1).bool(), float("-inf")), 1)
+    # one rounding of each weight and of the result; a score is off by dh + 8 float32 steps of its
+    # absolute terms, a sum of weights by n, both in numerator and denominator
+    u = R.unit(T)
+    terms = (q.double().abs() @ k.double().abs().t()).nan_to_num(posinf=0.0).amax(1, keepdim=True) * dh ** -0.5
+    bound = u * (p @ v.double()).abs() + (u + 2 * R.E * ((dh + 8) * terms + n)) * (p @ v.double().abs())
+    assert ((o.double() - p @ v.double()).abs() <= bound).all()
