@@ -342,7 +342,8 @@ mfmg_status mfmg_meta_grad_noalloc(mfmg_problem_t problem, const float* theta0,
  * hold anything) and output rows of theirs stay as they were.  Nothing of one sequence
  * enters another's results either, NaN and infinities included.  Within a sequence a
  * later token enters with weight 0, so one that is not finite may make earlier
- * tokens' results NaN.
+ * tokens' results NaN.  Scores of -inf are weights of 0; finite ones are resolved to
+ * float32, so beyond 2^30 in magnitude a row may come out as NaN.
  */
 /* How rotary frequencies theta_j = rope_base^(-2j / rope_dims), j < rope_dims / 2, are
  * stretched for contexts longer than those trained on, by rope_factor f >= 1:

@@ -39,6 +39,7 @@
 #include "packed.h"
 
 #include <algorithm>
+#include <cfloat>
 #include <type_traits>
 
 namespace mfmg {
@@ -338,7 +339,7 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<
     if constexpr (DUAL) qdf[c] = gfrag<NG>(a.qd + qc * a.ldqd + (long)h * dh, g, c, dh);
   }
   const float s2 = a.scale * 1.44269504088896341f;
-  float m = -INFINITY, l = 0.f, cs = 0.f;
+  float m = -FLT_MAX, l = 0.f, cs = 0.f;   // (finite: scores of -inf are weights of 0 from the start)
   V o[NE], od[DUAL ? NE : 1];
 #pragma unroll
   for (int e = 0; e < NE; ++e) {
@@ -401,7 +402,6 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<
       float mx = -INFINITY;
 #pragma unroll
       for (int t = 0; t < NS * AV; ++t) mx = fmaxf(mx, s[t / AV][t % AV]);
-      // the first keys hold a visible one of every query: m is finite from then on
       if (__any(mx * s2 > m + 8.f)) {
         const float mn = fmaxf(m, max_groups<R>(mx) * s2), al = exp2_(m - mn);
         m = mn;
@@ -459,7 +459,7 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<
       }
       __syncthreads();
       float f0 = 1.f, f1 = 1.f;
-      if (M.rank == 0) {   // (the first wave has seen the first key: its maximum is finite)
+      if (M.rank == 0) {
         const float m1 = M.scalar(0), mn = fmaxf(m, m1);
         f0 = exp2_(m - mn);
         f1 = exp2_(m1 - mn);
@@ -472,7 +472,7 @@ __global__ void __launch_bounds__(64 * NW, MW) packed_fwd_kernel(PackedAttnArgs<
     }
     if (M.rank) return;
   }
-  if (q >= hi) return;   // (lanes of one row leave together; q0 < hi has l > 0)
+  if (q >= hi) return;   // (lanes of one row leave together)
   const float lt = sum_groups<R>(l), inv = 1.0f / lt;
   const float c = DUAL ? sum_groups<R>(cs) * inv : 0.f;
   if (g == 0) {

@@ -356,3 +356,53 @@ def test_a_key_at_minus_infinity_has_no_weight(prec, dh):
     terms = (q.double().abs() @ k.double().abs().t()).nan_to_num(posinf=0.0).amax(1, keepdim=True) * dh ** -0.5
     bound = u * (p @ v.double()).abs() + (u + 2 * R.E * ((dh + 8) * terms + n)) * (p @ v.double().abs())
     assert ((o.double() - p @ v.double()).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("prec", [0, 1], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("n,first", [(70, 33), (300, 64), (300, 129)])
+def test_leading_keys_at_minus_infinity(prec, n, first):
+    """Whole blocks of keys at -inf before a query's first finite one: the finite ones' result; queries
+    that see no finite key are not a number, as softmax of a row of -inf is."""
+    print(f"\n[packed] {first} of {n} keys at -inf", flush=True)
+    M = _lib()
+    T, dh = torch.bfloat16 if prec else torch.float32, 64
+    op = M.Attention(M.make_attn_desc(heads=1, kv_heads=1, head_dim=dh, precision=prec))
+    whole, part = (M.mfmg_seq_plan(torch.tensor([0, m], dtype=torch.int32, device="cuda"), m)
+                   for m in (n, n - first))
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    q, k, v = (torch.randn(n, dh, device="cuda", generator=gen).to(T) for _ in range(3))
+    q[:, 0] = 1
+    k[:first, 0] = float("-inf")
+    o, o2 = torch.empty(n, dh, device="cuda", dtype=T), torch.empty(n - first, dh, device="cuda", dtype=T)
+    op.mfmg_attn_fwd(whole, q, k, v, o, torch.empty(2, 1, n, device="cuda"))
+    op.mfmg_attn_fwd(part, q[first:], k[first:], v[first:], o2, torch.empty(2, 1, n - first, device="cuda"))
+    torch.cuda.synchronize()
+    assert torch.isnan(o[:first]).all()
+    # the same weights in other blocks: two roundings of each and of the result, float32 steps of the scores
+    u, m = R.unit(T), n - first
+    terms = (q[first:].double().abs() @ k[first:].double().abs().t()).amax(1, keepdim=True) * dh ** -0.5
+    s = (q[first:].double() @ k[first:].double().t()) * dh ** -0.5
+    p = torch.softmax(s.masked_fill(torch.ones_like(s).triu(1).bool(), float("-inf")), 1)
+    a = p @ v[first:].double().abs()
+    bound = 2 * u * o2.double().abs() + 2 * (u + 2 * R.E * ((dh + 8) * terms + n)) * a
+    assert ((o[first:].double() - o2.double()).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("prec", [0, 1], ids=["fp32", "bf16"])
+def test_equal_scores_far_below_zero(prec):
+    """Scores of -2^120 on every key: the mean of the values seen."""
+    print("\n[packed] scores of -2^120", flush=True)
+    M = _lib()
+    n, dh, T = 50, 64, torch.bfloat16 if prec else torch.float32
+    op = M.Attention(M.make_attn_desc(heads=1, kv_heads=1, head_dim=dh, precision=prec, scale=1.0))
+    plan = M.mfmg_seq_plan(torch.tensor([0, n], dtype=torch.int32, device="cuda"), n)
+    q, k = (torch.zeros(n, dh, device="cuda", dtype=T) for _ in range(2))
+    q[:, 3], k[:, 3] = 2.0 ** 60, -2.0 ** 60
+    v = torch.randn(n, dh, device="cuda", generator=torch.Generator(device="cuda").manual_seed(3)).to(T)
+    o = torch.empty(n, dh, device="cuda", dtype=T)
+    op.mfmg_attn_fwd(plan, q, k, v, o, torch.empty(2, 1, n, device="cuda"))
+    torch.cuda.synchronize()
+    count = torch.arange(1, n + 1, device="cuda", dtype=torch.float64)[:, None]
+    want, a = v.double().cumsum(0) / count, v.double().abs().cumsum(0) / count
+    # (weights of 1 are exact) one rounding of the result, n + 4 float32 steps of the sums
+    assert ((o.double() - want).abs() <= R.unit(T) * want.abs() + (n + 4) * R.E * a).all()
